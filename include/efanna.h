@@ -64,6 +64,7 @@ typedef enum {
 #define EFANNA_MAX_SAMPLE 64    /* NN-descent sample size L                            */
 #define EFANNA_MAX_LEAF 64      /* leaf population S                                   */
 #define EFANNA_MAX_TREES 64
+#define EFANNA_MX_MAX_D 65536   /* coordinates of a row of an MXFP4 table              */
 /* size of the fixed device array behind efanna_nndescent_noalloc (64 MiB per GPU in use) */
 #define EFANNA_NOALLOC_SCRATCH_BYTES (64u << 20)
 
@@ -295,6 +296,64 @@ int efanna_search(const float *X, int64_t n, int32_t d, const int32_t *perm,
                   const int32_t *graph_ids, int32_t graph_k, const float *queries, int64_t nq,
                   int32_t k, int32_t pool, int32_t expand, int32_t iters, int32_t *ids,
                   float *dists, int32_t *checked, void *ws, size_t ws_bytes, void *stream);
+
+/* ---- vectors in microscaled 4-bit floating point ---------------------------------------------
+ * A table in MXFP4 takes 17/128 of its float32 rows' bytes and is what the matrix units multiply
+ * fastest.  It serves whoever scores or searches all rows: for the truth that a graph is compared
+ * with, for small sets, for first candidates that the float32 rows decide on.
+ *
+ * Format.  Coordinates of a row in blocks of 32, nb = ceil(d / 32) of them, the last one filled up
+ * with zeros.  A block holds a scale byte b, which stands for 2^(b - 127), and 32 codes of four
+ * bits: a sign and 0, 0.5, 1, 1.5, 2, 3, 4 or 6 (code 0..7; 8..15 are their negatives).
+ *   codes  n * 16 * nb bytes, 16-byte aligned: byte j of a row holds coordinate 2j in its low and
+ *          2j + 1 in its high four bits.
+ *   scales n * sp bytes, sp = nb rounded up to a multiple of 4, 4-byte aligned; padding bytes 0.
+ *   norms  n float32: squared length of the row as held; NaN if a scale byte of the row is 255.
+ * 1 <= d <= EFANNA_MX_MAX_D, n < 2^31 - 65536.  Row counts may be 0 (the call then does nothing;
+ * pointers to what has no elements may be NULL).  Element types of other matrices: EFANNA_F32,
+ * EFANNA_F16 (IEEE half) or EFANNA_BF16, aligned to their size.  All calls are asynchronous on
+ * `stream`, can be captured into a graph, and allocate nothing. */
+#define EFANNA_F32 0
+#define EFANNA_F16 1
+#define EFANNA_BF16 2
+
+/* Rows of X [device] (n rows of d elements of type dtype, ldx >= d elements apart) to a table.
+ * A block's scale is 2^(floor(log2 of its largest magnitude) - 2), 2^-127 at least (a block of
+ * zeros has that); a code is the nearest value of x / scale, ties to the even code, 6 at most.
+ * A block that holds an infinity or a NaN gets scale byte 255 and codes 0: all of it reads as NaN. */
+int efanna_mx_quantise(const void *X, int32_t dtype, int64_t n, int32_t d, int64_t ldx, uint8_t *codes,
+                       uint8_t *scales, float *norms, void *stream);
+
+/* Rows of a table by id: out[i] = factor * row ids[i], m rows of d elements, dense.
+ * ids    [device] m int32, or NULL: rows 0 .. m - 1 (m <= n).  An id below 0 or of n and more names an
+ *        empty slot, as in rows of efanna_get_graph: a row of zeros.
+ * Values are multiplied in float32 and rounded once (to nearest, ties to even). */
+int efanna_mx_rows(const uint8_t *codes, const uint8_t *scales, int64_t n, int32_t d, const int32_t *ids,
+                   int64_t m, float factor, int32_t dtype, void *out, void *stream);
+
+/* out[i * ldo + j] = a_i . b_j for the m rows of one table and the n rows of another, ldo >= n.
+ * Summed in float32 by the matrix units, rounded once to dtype. */
+int efanna_mx_product(const uint8_t *a_codes, const uint8_t *a_scales, int64_t m, const uint8_t *b_codes,
+                      const uint8_t *b_scales, int64_t n, int32_t d, int32_t dtype, void *out, int64_t ldo,
+                      void *stream);
+
+/* For each of nq rows q of one table the k rows x of another that come first in the order
+ * (s descending, id ascending), s = q.x - |x|^2 / 2 in float32 with |x|^2 taken from norms.
+ * That is the order (squared distance, id) of the rows as held, up to the rounding of s; s is exact
+ * wherever the terms of a sum span no more than 24 bits.
+ * norms, q_norms [device] as efanna_mx_quantise writes them (norms 16-byte aligned).  A row whose
+ *        norm is not finite is nobody's neighbour, a query whose norm is not finite has none.
+ * first_self >= 0: query i is row first_self + i of the table and not its own neighbour; -1: none is.
+ * ids, dists [device] out, nq * k int32 / float32: ids and max(0, |q|^2 - 2 s), nearest first; -1 and
+ *        +inf where there are fewer than k.
+ * Limits: 1 <= k <= EFANNA_MAX_K.  The workspace holds at most about 1 GiB (more queries take several
+ * passes; at least 256 queries go together, which beyond 15 * 10^6 rows takes more). */
+size_t efanna_mx_nearest_workspace_bytes(int64_t n, int64_t nq, int32_t k);
+
+int efanna_mx_nearest(const uint8_t *codes, const uint8_t *scales, const float *norms, int64_t n, int32_t d,
+                      const uint8_t *q_codes, const uint8_t *q_scales, const float *q_norms, int64_t nq,
+                      int32_t k, int64_t first_self, int32_t *ids, float *dists, void *ws, size_t ws_bytes,
+                      void *stream);
 
 #ifdef __cplusplus
 }

@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from typing import NamedTuple
 
 import numpy as np
 import torch
@@ -23,7 +24,8 @@ STATUS = {0: "EFANNA_OK", -1: "EFANNA_EINVAL", -2: "EFANNA_EWORKSPACE", -3: "EFA
 SYMBOLS = ["efanna_status_string", "efanna_trees_workspace_bytes", "efanna_build_trees", "efanna_build_trees_rule",
            "efanna_init_workspace_bytes", "efanna_init_graph", "efanna_nndescent_workspace_bytes",
            "efanna_nndescent", "efanna_nndescent_noalloc", "efanna_get_graph", "efanna_set_graph", "efanna_pair_distances",
-           "efanna_search_workspace_bytes", "efanna_search"]
+           "efanna_search_workspace_bytes", "efanna_search", "efanna_mx_quantise", "efanna_mx_rows", "efanna_mx_product",
+           "efanna_mx_nearest_workspace_bytes", "efanna_mx_nearest"]
 
 
 class EfannaError(RuntimeError):
@@ -72,6 +74,16 @@ def lib():
         L.efanna_search.restype = C.c_int
         L.efanna_search.argtypes = [vp, i64, i32, vp, vp, i32, vp, vp, i32, i32, i32, vp, i32, vp, i64,
                                     i32, i32, i32, i32, vp, vp, vp, vp, sz, vp]
+        L.efanna_mx_quantise.restype = C.c_int
+        L.efanna_mx_quantise.argtypes = [vp, i32, i64, i32, i64, vp, vp, vp, vp]
+        L.efanna_mx_rows.restype = C.c_int
+        L.efanna_mx_rows.argtypes = [vp, vp, i64, i32, vp, i64, C.c_float, i32, vp, vp]
+        L.efanna_mx_product.restype = C.c_int
+        L.efanna_mx_product.argtypes = [vp, vp, i64, vp, vp, i64, i32, i32, vp, i64, vp]
+        L.efanna_mx_nearest_workspace_bytes.restype = sz
+        L.efanna_mx_nearest_workspace_bytes.argtypes = [i64, i64, i32]
+        L.efanna_mx_nearest.restype = C.c_int
+        L.efanna_mx_nearest.argtypes = [vp, vp, vp, i64, i32, vp, vp, vp, i64, i32, i64, vp, vp, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -296,3 +308,106 @@ def efanna_search(X: torch.Tensor, perm: torch.Tensor, leaf_off: torch.Tensor, n
                                Q.data_ptr(), nq, k, pool, expand, iters, ids.data_ptr(), dists.data_ptr(),
                                checked.data_ptr(), ws.data_ptr(), ws.numel(), _stream()), "efanna_search")
     return ids, dists, checked
+
+
+class MxTable(NamedTuple):
+    """Vectors in MXFP4 (the format is described in efanna.h): codes [n, 16 * ceil(d / 32)] and scales
+    [n, ceil(d / 32) rounded up to 4] uint8, norms [n] float32, all on the device; d coordinates."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+    norms: torch.Tensor
+    d: int
+
+
+_MX_DTYPE = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+
+
+def _mx_dtype(dtype: torch.dtype) -> int:
+    if dtype not in _MX_DTYPE:
+        raise ValueError(f"expected float32, float16 or bfloat16, got {dtype}")
+    return _MX_DTYPE[dtype]
+
+
+def _mx_table(t: MxTable) -> int:
+    """Checks a table's tensors against one another; returns its row count."""
+    n, nb = t.codes.shape[0], (t.d + 31) // 32
+    _dev(t.codes, torch.uint8), _dev(t.scales, torch.uint8), _dev(t.norms, torch.float32)
+    if t.codes.shape != (n, 16 * nb) or t.scales.shape != (n, (nb + 3) // 4 * 4) or t.norms.shape != (n,):
+        raise ValueError("codes, scales and norms do not make a table of d coordinates")
+    if t.codes.device != t.scales.device or t.codes.device != t.norms.device:
+        raise ValueError("a table's tensors are on different devices")
+    return n
+
+
+def _mx_out(out: torch.Tensor | None, shape, dtype: torch.dtype, device) -> torch.Tensor:
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if out.device != device or out.dtype != dtype or out.shape != shape or (shape[1] > 1 and out.stride(1) != 1):
+        raise ValueError(f"out is not a {tuple(shape)} matrix of {dtype} with dense rows on {device}")
+    return out
+
+
+def efanna_mx_quantise(X: torch.Tensor) -> MxTable:
+    """Rows of X [n, d] (float32, float16 or bfloat16; rows may be further apart than d) as a table."""
+    code = _mx_dtype(X.dtype)
+    if not X.is_cuda or X.dim() != 2 or (X.numel() > 0 and X.shape[1] > 1 and X.stride(1) != 1):
+        raise ValueError("expected a device matrix with dense rows")
+    n, d = X.shape
+    ldx = X.stride(0) if n > 1 else d
+    nb = (d + 31) // 32
+    codes = torch.empty((n, 16 * nb), dtype=torch.uint8, device=X.device)
+    scales = torch.empty((n, (nb + 3) // 4 * 4), dtype=torch.uint8, device=X.device)
+    norms = torch.empty((n,), dtype=torch.float32, device=X.device)
+    _check(lib().efanna_mx_quantise(X.data_ptr(), code, n, d, ldx, codes.data_ptr(), scales.data_ptr(), norms.data_ptr(),
+                                    _stream()), "efanna_mx_quantise")
+    return MxTable(codes, scales, norms, d)
+
+
+def efanna_mx_rows(table: MxTable, ids: torch.Tensor | None = None, factor: float = 1.0,
+                   dtype: torch.dtype = torch.float32) -> torch.Tensor:
+    """factor * rows `ids` (int32, any shape; all rows if None) of a table, [*ids.shape, d]; zeros for ids that
+    are below 0 (empty slots of a graph) or not below the row count."""
+    code, n = _mx_dtype(dtype), _mx_table(table)
+    if ids is not None:
+        ids = _dev(ids, torch.int32)
+        if ids.device != table.codes.device:
+            raise ValueError("ids and table are on different devices")
+    m = n if ids is None else ids.numel()
+    out = torch.empty((m, table.d), dtype=dtype, device=table.codes.device)
+    _check(lib().efanna_mx_rows(table.codes.data_ptr(), table.scales.data_ptr(), n, table.d,
+                                None if ids is None else ids.data_ptr(), m, float(factor), code, out.data_ptr(), _stream()),
+           "efanna_mx_rows")
+    return out if ids is None else out.view(*ids.shape, table.d)
+
+
+def efanna_mx_product(a: MxTable, b: MxTable, dtype: torch.dtype = torch.float32,
+                      out: torch.Tensor | None = None) -> torch.Tensor:
+    """a_i . b_j for all rows of two tables, [rows of a, rows of b].  `out` may have rows that are further
+    apart than they are long."""
+    code, m, n = _mx_dtype(dtype), _mx_table(a), _mx_table(b)
+    if a.d != b.d or a.codes.device != b.codes.device:
+        raise ValueError("the tables differ in their dimension or device")
+    out = _mx_out(out, (m, n), dtype, a.codes.device)
+    ldo = out.stride(0) if m > 1 else max(n, 1)
+    _check(lib().efanna_mx_product(a.codes.data_ptr(), a.scales.data_ptr(), m, b.codes.data_ptr(), b.scales.data_ptr(), n,
+                                   a.d, code, out.data_ptr(), ldo, _stream()), "efanna_mx_product")
+    return out
+
+
+def efanna_mx_nearest(table: MxTable, queries: MxTable, k: int, first_self: int = -1,
+                      workspace: torch.Tensor | None = None):
+    """The k nearest rows of `table` to every row of `queries`, all rows compared: (ids [nq, k] int32, dists [nq, k]
+    float32, squared distances of the rows as held), nearest first, equal ones by id; -1 and +inf where there are
+    fewer.  first_self >= 0: query i is row first_self + i of the table and not its own neighbour."""
+    n, nq = _mx_table(table), _mx_table(queries)
+    if table.d != queries.d or table.codes.device != queries.codes.device:
+        raise ValueError("the tables differ in their dimension or device")
+    device = table.codes.device
+    ids = torch.empty((nq, max(k, 0)), dtype=torch.int32, device=device)
+    dists = torch.empty((nq, max(k, 0)), dtype=torch.float32, device=device)
+    ws = _workspace(lib().efanna_mx_nearest_workspace_bytes(n, nq, k), device) if workspace is None else workspace
+    _check(lib().efanna_mx_nearest(table.codes.data_ptr(), table.scales.data_ptr(), table.norms.data_ptr(), n, table.d,
+                                   queries.codes.data_ptr(), queries.scales.data_ptr(), queries.norms.data_ptr(), nq, k,
+                                   int(first_self), ids.data_ptr(), dists.data_ptr(), ws.data_ptr(), ws.numel(), _stream()),
+           "efanna_mx_nearest")
+    return ids, dists

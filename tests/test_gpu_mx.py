@@ -1,0 +1,486 @@
+"""MXFP4 tables on the GPU (quantisation, rows by id, products, nearest rows) against a plain statement of
+the format and of the operators in 64 bits.  Codes, scales, ids and everything that float32 holds exactly are
+compared exactly; other values within bounds that count roundings (half a step each)."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+GRID = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+TYPES = [torch.float32, torch.float16, torch.bfloat16]
+
+
+@pytest.fixture(scope="module")
+def ef():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a GPU: there is no CPU fallback")
+    from paper_1609_07228_amd import efanna
+    return efanna
+
+
+# ---- the plain statement ---------------------------------------------------------------------------------
+
+
+def ref_quantise(x):
+    """codes [n, 16 nb], scales [n, sp] of float64 rows, by the nearest grid value (ties: even code)."""
+    n, d = x.shape
+    nb, sp = (d + 31) // 32, ((d + 31) // 32 + 3) // 4 * 4
+    full = np.zeros((n, nb * 32))
+    full[:, :d] = x
+    blocks = full.reshape(n, nb, 32)
+    codes = np.zeros((n, nb, 32), np.uint8)
+    scales = np.zeros((n, sp), np.uint8)
+    for b in range(nb):
+        v = blocks[:, b]
+        with np.errstate(all="ignore"):
+            top = np.abs(v).max(axis=1)
+            bad = ~np.isfinite(top) | np.isnan(v).any(axis=1)
+            e = np.where((top > 0) & ~bad, np.floor(np.log2(np.where((top > 0) & ~bad, top, 1.0))), -200) - 2
+        # log2 of float64 is not trusted next to a power of two
+        with np.errstate(all="ignore"):
+            e = np.where(top >= 2.0 ** (e + 3), e + 1, e)
+            e = np.where((top < 2.0 ** (e + 2)) & (top > 0), e - 1, e)
+        e = np.maximum(e, -127)
+        with np.errstate(all="ignore"):
+            r = np.abs(v) / (2.0 ** e)[:, None]
+            r[bad] = 0
+        away = np.abs(r[:, :, None] - GRID)
+        best = away.min(axis=2, keepdims=True)
+        pick = away == best                     # one or two grid values
+        even = pick & (np.arange(8) % 2 == 0)
+        code = np.where(pick.sum(axis=2) == 2, even.argmax(axis=2), pick.argmax(axis=2)).astype(np.uint8)
+        code |= (np.signbit(v) & ~bad[:, None]).astype(np.uint8) << 3
+        codes[:, b] = code
+        scales[:, b] = np.where(bad, 255, e + 127)
+    flat = codes.reshape(n, nb * 32)
+    return flat[:, 0::2] | (flat[:, 1::2] << 4), scales
+
+
+def ref_held(codes, scales, d):
+    value = np.concatenate([GRID, -GRID])
+    n, nb = codes.shape[0], (d + 31) // 32
+    v = np.stack([value[codes & 15], value[codes >> 4]], axis=2).reshape(n, nb, 32)
+    p = 2.0 ** (scales[:, :nb].astype(np.float64) - 127)
+    p[scales[:, :nb] == 255] = np.nan
+    return (v * p[:, :, None]).reshape(n, nb * 32)[:, :d]
+
+
+def ref_nearest(X, Q, k, first_self=-1):
+    """(ids, dists) by (distance, id) in float64; rows and queries with a norm outside float32 take no part."""
+    xx, qq = (X * X).sum(axis=1), (Q * Q).sum(axis=1)
+    ids = np.full((len(Q), k), -1, np.int32)
+    dists = np.full((len(Q), k), np.inf)
+    limit = float(np.finfo(np.float32).max)
+    for i in range(len(Q)):
+        if not qq[i] <= limit:
+            continue
+        dist = np.maximum(qq[i] + xx - 2.0 * (X @ Q[i]), 0.0)
+        ok = xx <= limit
+        if first_self >= 0 and first_self + i < len(X):
+            ok[first_self + i] = False
+        at = np.nonzero(ok)[0]
+        at = at[np.argsort(dist[at], kind="stable")][:k]
+        ids[i, :len(at)], dists[i, :len(at)] = at, dist[at]
+    return ids, dists
+
+
+def float32_is_exact(X, Q):
+    """Whether every sum behind s and the distances is a multiple of one unit and below 2^24 of it."""
+    with np.errstate(divide="ignore"):
+        ux, uq = (min((np.spacing(np.abs(v[v != 0])) * 2.0 ** 51).min(initial=1.0), 1.0) for v in (X, Q))
+    unit = min(ux * uq, ux * ux / 2, uq * uq)              # a held value has two bits: its second one is 2^-51 / 2^-52 of it
+    xx, qq = (X * X).sum(axis=1).max(initial=0.0), (Q * Q).sum(axis=1).max(initial=0.0)
+    return (qq + 2 * np.sqrt(xx * qq) + xx) / unit < 2.0 ** 24
+
+
+def check_nearest(got, X, Q, k, first_self=-1):
+    """Equal to the definition where float32 is exact; otherwise every id and distance within the roundings:
+    s is a sum of at most d + d / 32 + 1 terms, |q|^2 of d, and the distance adds one more, half a step each."""
+    ids, dists = host(got[0]), host(got[1])
+    want_ids, want_dists = ref_nearest(X, Q, k, first_self)
+    if float32_is_exact(X, Q):
+        assert np.array_equal(ids, want_ids) and np.array_equal(dists, want_dists)
+        return
+    d = X.shape[1]
+    xx, qq = (X * X).sum(axis=1), (Q * Q).sum(axis=1)
+    for i in range(len(Q)):
+        live = int((want_ids[i] >= 0).sum())
+        assert (ids[i, live:] == -1).all() and np.isinf(dists[i, live:]).all()
+        at = ids[i, :live]
+        assert len(set(at)) == live and (at >= 0).all() and not (first_self >= 0 and first_self + i in at)
+        room = 2 * (d + d / 32 + 4) * 2.0 ** -24 * (np.abs(X) @ np.abs(Q[i]) + xx / 2 + qq[i])
+        dist = np.maximum(qq[i] + xx - 2 * (X @ Q[i]), 0)
+        assert np.all(np.abs(dists[i, :live] - dist[at]) <= room[at])
+        assert np.all(np.diff(dists[i, :live]) >= 0)
+        if live == k:                                       # nothing that is certainly nearer was missed
+            rest = np.ones(len(X), bool)
+            rest[at] = False
+            if first_self >= 0 and first_self + i < len(X):
+                rest[first_self + i] = False
+            assert np.all(dist[rest] + room[rest] >= dist[at[-1]] - room[at[-1]])
+
+
+def host(t):
+    return t.detach().cpu().to(torch.float64).numpy() if t.dtype.is_floating_point else t.cpu().numpy()
+
+
+def table(ef, x, dtype=torch.float32):
+    """A table on the device and its rows as held, float64."""
+    t = ef.efanna_mx_quantise(torch.as_tensor(x).to(dtype).cuda())
+    return t, ref_held(host(t.codes), host(t.scales), t.d)
+
+
+def vectors(rng, n, d, kind="gauss"):
+    if kind == "gauss":
+        return rng.standard_normal((n, d)).astype(np.float32)
+    if kind == "grid":            # small integers: many equal distances
+        return rng.integers(-2, 3, (n, d)).astype(np.float32)
+    if kind == "u8":
+        return rng.integers(0, 256, (n, d)).astype(np.float32)
+    return (rng.standard_normal((n, d)) * np.exp2(rng.integers(-3, 4, (n, 1)))).astype(np.float32)      # "wide"
+
+
+# ---- quantisation ------------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "f16", "bf16"])
+@pytest.mark.parametrize("n,d,pad", [(1, 1, 0), (1, 32, 0), (3, 7, 0), (5, 31, 2), (64, 128, 0), (70, 33, 1), (257, 50, 7),
+                                     (129, 96, 0), (33, 129, 3), (17, 200, 8), (9, 960, 0), (4, 1025, 5), (2, 4097, 0),
+                                     (1001, 16, 0), (300, 8, 0), (3, 65536, 0)])
+def test_quantise_codes_scales_and_norms(ef, dtype, n, d, pad):
+    rng = np.random.default_rng(n * 7919 + d)
+    wide = torch.zeros((n, d + pad), dtype=dtype, device="cuda")
+    wide[:, :d] = torch.from_numpy(vectors(rng, n, d, "wide")).to(dtype).cuda()
+    if pad:
+        wide[:, d:] = float("nan")        # what lies between the rows is not theirs
+    x = wide[:, :d]
+    t = ef.efanna_mx_quantise(x)
+    codes, scales = ref_quantise(host(x))
+    assert np.array_equal(host(t.codes), codes)
+    assert np.array_equal(host(t.scales), scales)
+    held = ref_held(codes, scales, d)
+    want = (held * held).sum(axis=1)
+    # a sum of d non-negative terms, added in some order: at most d roundings of half a step, relative
+    assert np.all(np.abs(host(t.norms) - want) <= d * 2.0 ** -24 * want)
+
+
+@pytest.mark.parametrize("shift", [0, 1, 3])
+def test_quantise_rows_at_any_element_alignment(ef, shift):
+    rng = np.random.default_rng(shift)
+    for dtype in TYPES:
+        buf = torch.zeros(5000, dtype=dtype, device="cuda")
+        buf[shift:shift + 40 * 67] = torch.from_numpy(rng.standard_normal(40 * 67).astype(np.float32)).to(dtype).cuda()
+        x = buf[shift:shift + 40 * 67].view(40, 67)[:, :65]
+        t = ef.efanna_mx_quantise(x)
+        codes, scales = ref_quantise(host(x))
+        assert np.array_equal(host(t.codes), codes) and np.array_equal(host(t.scales), scales)
+
+
+def test_quantise_ties_borders_and_ends(ef):
+    # every border of the grid and its neighbours in float32, under several powers of two; 4 fixes the scale
+    borders = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0, 7.0], np.float32)
+    vals = np.concatenate([borders, np.nextafter(borders, np.float32(9)), np.nextafter(borders, np.float32(0))])
+    vals = np.concatenate([vals, -vals])
+    rows = []
+    for p in (-100, -20, 0, 20, 100):
+        for v in vals:
+            r = np.zeros(32, np.float32)
+            r[0], r[5] = 4.0, v
+            rows.append(r * np.float32(2.0) ** p)
+    x = np.stack(rows)
+    t = ef.efanna_mx_quantise(torch.from_numpy(x).cuda())
+    codes, scales = ref_quantise(x.astype(np.float64))
+    assert np.array_equal(host(t.codes), codes) and np.array_equal(host(t.scales), scales)
+
+
+def test_quantise_zeros_tiny_huge_and_non_finite(ef):
+    tiny = np.float32(1e-45)
+    rows = np.zeros((12, 70), np.float32)
+    rows[1, 3] = -0.0
+    rows[2, :] = tiny
+    rows[3, 40] = np.float32(2.0) ** -126
+    rows[4, 2] = np.finfo(np.float32).max
+    rows[5, 2:9] = [1, 2, np.inf, 3, 0, 0, 1]
+    rows[6, 33] = np.nan
+    rows[7, 69] = -np.inf
+    rows[8, :] = np.float32(3.3) * np.float32(2.0) ** -127
+    rows[9, :] = 1.0
+    rows[10, 64:] = -5.0
+    t = ef.efanna_mx_quantise(torch.from_numpy(rows).cuda())
+    codes, scales = ref_quantise(rows.astype(np.float64))
+    assert np.array_equal(host(t.codes), codes) and np.array_equal(host(t.scales), scales)
+    norms = host(t.norms)
+    assert np.isnan(norms[[5, 6, 7]]).all() and np.isfinite(norms[[0, 1, 2, 3, 8, 9, 10, 11]]).all()
+    assert norms[4] == np.inf
+    back = host(ef.efanna_mx_rows(t))
+    want = ref_held(codes, scales, 70)
+    assert np.array_equal(back, want, equal_nan=True)
+    assert np.isnan(back[5, :32]).all() and (back[5, 32:] == 0).all()
+
+
+# ---- rows --------------------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "f16", "bf16"])
+@pytest.mark.parametrize("n,d,m", [(1, 1, 1), (5, 7, 40), (100, 32, 3), (64, 50, 999), (33, 128, 257), (20, 129, 65),
+                                   (7, 1000, 31), (300, 16, 2000), (2, 4100, 5)])
+def test_rows_by_id(ef, dtype, n, d, m):
+    rng = np.random.default_rng(n + d + m)
+    t, held = table(ef, vectors(rng, n, d))
+    ids = rng.integers(0, n, m).astype(np.int32)
+    ids[rng.random(m) < 0.2] = -1
+    if m > 4:
+        ids[:4] = [n, -2147483648, 2147483647, n - 1]
+    got = host(ef.efanna_mx_rows(t, torch.from_numpy(ids).cuda(), factor=0.3, dtype=dtype))
+    live = (ids >= 0) & (ids < n)
+    want = np.where(live[:, None], held[np.where(live, ids, 0)] * float(np.float32(0.3)), 0.0)
+    # the product in float32, then the rounding to dtype: half a step each (subnormal halves: half of 2^-24)
+    eps = 2.0 ** -24 + (torch.finfo(dtype).eps / 2 if dtype != torch.float32 else 0.0)
+    assert np.all(np.abs(got - want) <= 1.01 * eps * np.abs(want) + (2.0 ** -25 if dtype == torch.float16 else 0.0))
+    # all rows, factor 1: what a type holds of them exactly (codes have two significant bits)
+    assert np.array_equal(host(ef.efanna_mx_rows(t, dtype=dtype)), held)
+
+
+def test_rows_of_a_graph_keep_its_shape(ef):
+    rng = np.random.default_rng(5)
+    t, held = table(ef, vectors(rng, 50, 40))
+    ids = torch.from_numpy(rng.integers(-1, 50, (9, 4)).astype(np.int32)).cuda()
+    got = ef.efanna_mx_rows(t, ids)
+    assert got.shape == (9, 4, 40)
+    assert np.array_equal(host(got), np.where(host(ids)[:, :, None] < 0, 0.0, held[host(ids)]))
+    assert ef.efanna_mx_rows(t, ids[:0]).shape == (0, 4, 40)
+
+
+# ---- product -----------------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "f16", "bf16"])
+@pytest.mark.parametrize("m,n,d", [(1, 1, 1), (1, 16, 32), (1, 1000, 128), (2, 77, 50), (15, 300, 96), (16, 129, 129),
+                                   (17, 64, 256), (33, 65, 1000), (64, 1, 160), (100, 257, 33), (129, 130, 544),
+                                   (256, 256, 512), (300, 513, 640), (1, 100, 4128), (5, 33, 8192), (257, 1025, 128)])
+def test_product(ef, dtype, m, n, d):
+    rng = np.random.default_rng(m * 31 + n * 7 + d)
+    a, ah = table(ef, vectors(rng, m, d))
+    b, bh = table(ef, vectors(rng, n, d, "wide"))
+    got = host(ef.efanna_mx_product(a, b, dtype=dtype))
+    want = ah @ bh.T
+    # float32 sums of at most d + d / 32 roundings, each at most half a step of the sum of magnitudes; then one to dtype
+    room = (d + d / 32 + 2) * 2.0 ** -24 * (np.abs(ah) @ np.abs(bh).T)
+    if dtype != torch.float32:
+        room = room + 1.01 * torch.finfo(dtype).eps / 2 * (np.abs(want) + room) + (2.0 ** -25 if dtype == torch.float16 else 0)
+    assert np.all(np.abs(got - want) <= room)
+
+
+@pytest.mark.parametrize("m,n,d", [(3, 200, 128), (130, 200, 960), (300, 300, 1504), (16, 5000, 96)])
+def test_product_is_exact_where_float32_is(ef, m, n, d):
+    rng = np.random.default_rng(d)
+    a, ah = table(ef, vectors(rng, m, d, "u8"))
+    b, bh = table(ef, vectors(rng, n, d, "u8"))
+    assert np.array_equal(host(ef.efanna_mx_product(a, b)), ah @ bh.T)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "f16", "bf16"])
+@pytest.mark.parametrize("m,n,pad", [(1, 50, 3), (20, 33, 1), (140, 200, 8), (300, 260, 5)])
+def test_product_into_a_wider_matrix(ef, dtype, m, n, pad):
+    rng = np.random.default_rng(n)
+    a, ah = table(ef, vectors(rng, m, 64, "grid"))
+    b, bh = table(ef, vectors(rng, n, 64, "grid"))
+    wide = torch.full((m + 1, n + pad), 7.0, dtype=dtype, device="cuda")
+    out = wide[:m, :n]
+    assert ef.efanna_mx_product(a, b, dtype=dtype, out=out) is out
+    got = host(wide)
+    assert np.array_equal(got[:m, :n], ah @ bh.T)
+    assert (got[m:] == 7).all() and (got[:, n:] == 7).all()
+
+
+def test_product_with_rows_that_are_not_numbers(ef):
+    x = np.ones((40, 64), np.float32)
+    x[3, 5] = np.nan
+    x[39, 40] = np.inf
+    t = ef.efanna_mx_quantise(torch.from_numpy(x).cuda())
+    got = host(ef.efanna_mx_product(t, t))
+    bad = np.zeros(40, bool)
+    bad[[3, 39]] = True
+    assert np.isnan(got[bad]).all() and np.isnan(got[:, bad]).all()
+    assert (got[~bad][:, ~bad] == 64.0).all()
+
+
+def test_product_beyond_two_to_the_31_elements(ef):
+    rng = np.random.default_rng(2)
+    m, n, d = 4100, 530_000, 32                         # 2.17 * 10^9 outputs
+    a, ah = table(ef, vectors(rng, m, d, "grid"))
+    b, bh = table(ef, vectors(rng, n, d, "grid"))
+    got = ef.efanna_mx_product(a, b, dtype=torch.bfloat16)
+    for i in (0, 4051, 4052, 4099):
+        want = torch.from_numpy(ah[i] @ bh.T).to(torch.bfloat16)
+        assert torch.equal(got[i].cpu(), want)
+
+
+# ---- nearest -----------------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("kind", ["gauss", "grid", "u8"])
+@pytest.mark.parametrize("n,nq,d,k", [(1, 1, 1, 1), (1, 3, 40, 5), (10, 4, 32, 10), (100, 17, 50, 128), (255, 5, 128, 1),
+                                      (257, 33, 96, 7), (1000, 1, 128, 10), (1025, 65, 33, 16), (4000, 130, 64, 20),
+                                      (5003, 2, 960, 100), (3000, 300, 8, 3), (20_000, 16, 128, 128), (2500, 7, 1100, 9),
+                                      (70_001, 3, 16, 12), (40_000, 515, 32, 10)])
+def test_nearest(ef, kind, n, nq, d, k):
+    rng = np.random.default_rng(n + nq + d + k)
+    t, X = table(ef, vectors(rng, n, d, kind))
+    q, Q = table(ef, vectors(rng, nq, d, kind))
+    check_nearest(ef.efanna_mx_nearest(t, q, k), X, Q, k)
+
+
+@pytest.mark.parametrize("n,d,k,first", [(300, 24, 5, 0), (2000, 64, 30, 0), (2000, 64, 128, 1990), (1, 8, 2, 0), (500, 8, 4, 200)])
+def test_nearest_of_own_rows_leaves_each_out(ef, n, d, k, first):
+    rng = np.random.default_rng(n + first)
+    x = vectors(rng, n, d, "grid")
+    x[n // 2:] = x[:n - n // 2]                          # every vector twice: the other copy is its nearest
+    t, X = table(ef, x)
+    q, Q = table(ef, x[first:])
+    ids, dists = ef.efanna_mx_nearest(t, q, k, first_self=first)
+    want = ref_nearest(X, Q, k, first)
+    assert np.array_equal(host(ids), want[0]) and np.array_equal(host(dists), want[1])
+
+
+def test_nearest_when_all_rows_are_equal(ef):
+    t, X = table(ef, np.full((9000, 40), 1.5, np.float32))
+    q, Q = table(ef, np.full((3, 40), 1.5, np.float32))
+    ids, dists = ef.efanna_mx_nearest(t, q, 100)
+    assert np.array_equal(host(ids), np.tile(np.arange(100, dtype=np.int32), (3, 1))) and (host(dists) == 0).all()
+    ids, _ = ef.efanna_mx_nearest(t, q, 100, first_self=50)
+    for i in range(3):
+        assert np.array_equal(host(ids)[i], np.delete(np.arange(101), 50 + i))
+
+
+def test_nearest_leaves_out_what_is_not_finite(ef):
+    rng = np.random.default_rng(9)
+    x = vectors(rng, 3000, 40, "grid")
+    x[::7, 3] = np.nan
+    x[1::7, 39] = -np.inf
+    x[2::7, 5] = 1e30                                    # finite, but its square is not
+    x[3::7, 5] = 3e38
+    y = x[:21].copy()
+    t, X = table(ef, x)
+    q, Q = table(ef, y)
+    for k in (4, 128):
+        ids, dists = ef.efanna_mx_nearest(t, q, k)
+        want = ref_nearest(X, Q, k)
+        assert np.array_equal(host(ids), want[0]) and np.array_equal(host(dists), want[1])
+        assert (host(ids)[0] == -1).all() and np.isinf(host(dists)[0]).all()
+    # nothing but such rows
+    t, X = table(ef, x[::7].copy())
+    ids, dists = ef.efanna_mx_nearest(t, ef.efanna_mx_quantise(torch.zeros((2, 40), device="cuda")), 3)
+    assert (host(ids) == -1).all() and np.isinf(host(dists)).all()
+
+
+def test_nearest_without_rows_or_queries(ef):
+    none, _ = table(ef, np.zeros((0, 40), np.float32))
+    some, _ = table(ef, np.ones((5, 40), np.float32))
+    ids, dists = ef.efanna_mx_nearest(none, some, 3)
+    assert (host(ids) == -1).all() and np.isinf(host(dists)).all()
+    ids, dists = ef.efanna_mx_nearest(some, none, 3)
+    assert ids.shape == (0, 3) and dists.shape == (0, 3)
+
+
+def test_nearest_of_mixed_magnitudes_is_a_k_best_by_its_own_scores(ef):
+    """Rows of very different lengths: s is rounded, so the order is checked against distances within the bound
+    of those roundings, and that no row beyond the bound was missed."""
+    rng = np.random.default_rng(11)
+    n, d, k = 6000, 100, 10
+    x = (vectors(rng, n, d) * np.exp2(rng.integers(-12, 13, (n, 1)))).astype(np.float32)
+    t, X = table(ef, x)
+    q, Q = table(ef, x[:40])
+    assert not float32_is_exact(X, Q)
+    check_nearest(ef.efanna_mx_nearest(t, q, k), X, Q, k)
+
+
+def test_nearest_in_several_passes_and_on_a_given_workspace(ef):
+    """So many queries that the workspace holds some of them at a time."""
+    rng = np.random.default_rng(12)
+    n, nq = 300_000, 40_000
+    x = vectors(rng, n, 16, "grid")
+    t, X = table(ef, x)
+    y = vectors(rng, nq, 16, "grid")
+    q, Q = table(ef, y)
+    need = ef.lib().efanna_mx_nearest_workspace_bytes(n, nq, 6)
+    ws = torch.full((need + 512,), 0xA5, dtype=torch.uint8, device="cuda")
+    ids, dists = ef.efanna_mx_nearest(t, q, 6, workspace=ws[:need])
+    assert (host(ws[need:]) == 0xA5).all()
+    at = np.concatenate([np.arange(4), rng.integers(0, nq, 24), np.arange(nq - 4, nq)])
+    want = ref_nearest(X, Q[at], 6)
+    assert np.array_equal(host(ids)[at], want[0]) and np.array_equal(host(dists)[at], want[1])
+
+
+# ---- large tables, streams, graphs --------------------------------------------------------------------------
+
+
+def test_codes_beyond_four_gigabytes(ef):
+    """Rows whose codes start past 2^32 bytes are read where they are, by all readers."""
+    d, n = 2048, 4_300_000                               # 1 KiB of codes a row
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    codes = torch.randint(0, 256, (n, d // 2), generator=gen, device="cuda", dtype=torch.uint8)
+    scales = torch.randint(126, 129, (n, d // 32), generator=gen, device="cuda", dtype=torch.uint8)
+    at = np.array([0, 1, 2 ** 21, 2 ** 22 - 1, 2 ** 22, 2 ** 22 + 1, n - 2, n - 1], np.int32)
+    index = torch.from_numpy(at.astype(np.int64)).cuda()
+    some = ref_held(host(codes[index]), host(scales[index]), d)
+    norms = torch.full((n,), 1e9, device="cuda")
+    norms[index] = torch.from_numpy((some * some).sum(axis=1)).to(torch.float32).cuda()
+    t = ef.MxTable(codes, scales, norms, d)
+    assert np.array_equal(host(ef.efanna_mx_rows(t, torch.from_numpy(at).cuda())), some)
+    q = ef.MxTable(codes[index], scales[index], norms[index].contiguous(), d)
+    got = host(ef.efanna_mx_product(q, t)[:, index])
+    assert np.array_equal(got, some @ some.T)
+    ids, dists = ef.efanna_mx_nearest(t, q, 1)
+    assert np.array_equal(host(ids)[:, 0], at) and (host(dists) == 0).all()
+
+
+def test_on_a_stream_of_its_own(ef):
+    rng = np.random.default_rng(21)
+    x = vectors(rng, 5000, 96, "u8")
+    y = vectors(rng, 50, 96, "u8")
+    X, Y = torch.from_numpy(x).cuda(), torch.from_numpy(y).cuda()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        t, q = ef.efanna_mx_quantise(X), ef.efanna_mx_quantise(Y)
+        ids, dists = ef.efanna_mx_nearest(t, q, 9)
+        scores = ef.efanna_mx_product(q, t)
+        rows = ef.efanna_mx_rows(t, ids)
+    side.synchronize()
+    held = ref_held(host(t.codes), host(t.scales), 96)
+    qh = ref_held(host(q.codes), host(q.scales), 96)
+    want = ref_nearest(held, qh, 9)
+    assert np.array_equal(host(ids), want[0]) and np.array_equal(host(dists), want[1])
+    assert np.array_equal(host(scores), qh @ held.T)
+    assert np.array_equal(host(rows), held[want[0]])
+
+
+def test_captured_into_a_graph(ef):
+    rng = np.random.default_rng(22)
+    d, n, nq, k = 64, 3000, 20, 8
+    t, held = table(ef, vectors(rng, n, d, "u8"))
+    x = torch.zeros((nq, d), device="cuda")
+
+    def step():
+        q = ef.efanna_mx_quantise(x)
+        ids, dists = ef.efanna_mx_nearest(t, q, k)
+        return q.codes, q.scales, ids, dists, ef.efanna_mx_product(q, t), ef.efanna_mx_rows(t, ids, factor=0.5)
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = step()
+    for replay in range(4):
+        x.copy_(torch.from_numpy(vectors(rng, nq, d, "u8")).cuda())
+        graph.replay()
+        torch.cuda.synchronize()
+        codes, scales, ids, dists, scores, rows = (host(o) for o in outs)
+        eager = [host(o) for o in step()]
+        for got, same in zip((codes, scales, ids, dists, scores, rows), eager):
+            assert np.array_equal(got, same)
+        Q = ref_held(codes, scales, d)
+        want = ref_nearest(held, Q, k)
+        assert np.array_equal(ids, want[0]) and np.array_equal(dists, want[1])
+        assert np.array_equal(scores, Q @ held.T)
