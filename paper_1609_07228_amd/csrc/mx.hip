@@ -353,7 +353,7 @@ struct StageLds {
 };
 
 template <int KS, int QF>
-__global__ __launch_bounds__(512, 2) void scan_wide_kernel(Scan a)
+__global__ __launch_bounds__(512, KS == 1 ? 4 : 2) void scan_wide_kernel(Scan a)
 {
     typedef StageLds<KS> Lds;
     constexpr int TS = Lds::tiles, kOps = TS * KS;
@@ -555,186 +555,308 @@ __global__ __launch_bounds__(256) void scan_narrow_kernel(Scan a)
     }
 }
 
-struct PickShared {
-    u32 hist[256];
-    u32 waves[8];
-    u32 prefix, need, count;
-};
-
-// The `k` smallest of m words, ties by the lower index, as ascending indices in out; returns the last one's
-// word (the largest there is if m <= k) and their number.  All threads of the block take part; value(i) is called
-// for i < m only.
-template <int THREADS, class Value>
-__device__ u32 choose(Value value, int m, int k, int *out, PickShared &sh, int &count)
+// The `want`-th smallest of a wave's 64 * R words (want <= 64 * R), bit by bit; `less` of them are smaller.
+template <int R>
+__device__ inline u32 wave_nth(const u32 (&v)[R], int want, int &less)
 {
-    const int tid = threadIdx.x;
-    if (m <= k) {
-        for (int i = tid; i < m; i += THREADS) out[i] = i;
-        count = m;
-        __syncthreads();
-        return ~0u;
-    }
-    // the k-th smallest word, eight bits at a time from the top
-    u32 prefix = 0, need = k;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        for (int i = tid; i < 256; i += THREADS) sh.hist[i] = 0;
-        __syncthreads();
-        for (int i = tid; i < m; i += THREADS) {
-            const u32 v = value(i);
-            if (shift == 24 || (v >> (shift + 8)) == prefix) atomicAdd(&sh.hist[(v >> shift) & 255], 1u);
-        }
-        __syncthreads();
-        if (tid < 64) {        // lane l owns the digits 4 l .. 4 l + 3
-            u32 c[4], sum = 0;
+    u32 t = 0;
+    less = 0;
+    for (u32 bit = 0x80000000u; bit != 0; bit >>= 1) {
+        int n = 0;                         // words whose leading bits are t's with this bit 0: those below t + bit, less the smaller ones
 #pragma unroll
-            for (int j = 0; j < 4; ++j) sum += c[j] = sh.hist[4 * tid + j];
-            u32 upto = sum;
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const u32 other = (u32)__shfl_up((int)upto, o);
-                if (tid >= o) upto += other;
-            }
-            u32 before = upto - sum;
-            if (before < need && upto >= need)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (before < need && before + c[j] >= need) {
-                        sh.prefix = (prefix << 8) | (u32)(4 * tid + j);
-                        sh.need = need - before;
-                    }
-                    before += c[j];
-                }
+        for (int i = 0; i < R; ++i) n += __popcll(__ballot(v[i] < t + bit));
+        if (n < want) {
+            t += bit;
+            less = n;
         }
-        __syncthreads();
-        prefix = sh.prefix;
-        need = sh.need;
-        __syncthreads();
     }
-    // all that are smaller, and the first `need` of the equal ones, in the order of their indices
-    u32 equal_before = 0, before = 0;
-    const int lane = tid & 63, wave = tid >> 6;
-    const u64 below = (1ULL << lane) - 1;
-    for (int i0 = 0; i0 < m; i0 += THREADS) {
-        const int i = i0 + tid;
-        const u32 v = i < m ? value(i) : ~0u;
-        const u64 eq = __ballot(i < m && v == prefix);
-        if (lane == 0) sh.waves[wave] = (u32)__popcll(eq);
-        __syncthreads();
-        u32 eq_rank = equal_before + (u32)__popcll(eq & below);
-        for (int w = 0; w < THREADS / 64; ++w) {
-            if (w < wave) eq_rank += sh.waves[w];
-            equal_before += sh.waves[w];
-        }
-        const bool take = i < m && (v < prefix || (v == prefix && eq_rank < need));
-        const u64 taken = __ballot(take);
-        __syncthreads();
-        if (lane == 0) sh.waves[wave] = (u32)__popcll(taken);
-        __syncthreads();
-        u32 pos = before + (u32)__popcll(taken & below);
-        for (int w = 0; w < THREADS / 64; ++w) {
-            if (w < wave) pos += sh.waves[w];
-            before += sh.waves[w];
-        }
-        if (take) out[pos] = i;
-        __syncthreads();
-    }
-    count = k;
-    return prefix;
+    return t;
 }
 
-// One block per query.  LDS: keys (as many as the chosen groups have rows), then the values of the groups, then the lists.
-__global__ __launch_bounds__(256) void pick_kernel(Scan a, int k, long long first_self, int *ids, float *dists)
+// The smallest keys (word, index) that a wave has met, in LDS.  limit: a key that `want` keys of the list do not
+// exceed, once there are so many (all ones until then); nothing above it is taken in.
+constexpr int kListRoom = 512;             // entries beyond `want`
+struct KeyList {
+    u64 *keys;
+    int want, count;
+    u64 limit;
+    __device__ inline void start(u64 *at, int want_) { keys = at, want = want_, count = 0, limit = ~0ULL; }
+    // all lanes; room for 64 more is the caller's care
+    __device__ inline void push(u64 key, bool take, int lane)
+    {
+        take = take && key < limit;
+        const u64 mask = __ballot(take);
+        if (take) keys[count + __popcll(mask & ((1ULL << lane) - 1))] = key;
+        count += __popcll(mask);
+    }
+    // all of at most 64 * ROUNDS keys into ascending order, by their ranks, and down to `want`.  (Keys go from lane to
+    // lane through scalar registers: reading them from LDS in the loop, a wave waits for each.)
+    template <int ROUNDS> __device__ inline void sort_of(int lane)
+    {
+        u64 mine[ROUNDS];
+        int rank[ROUNDS];
+#pragma unroll
+        for (int i = 0; i < ROUNDS; ++i) {
+            mine[i] = i * 64 + lane < count ? keys[i * 64 + lane] : ~0ULL;
+            rank[i] = 0;
+        }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int b = 0; b < ROUNDS; ++b) {
+            const int n = min(count - b * 64, 64);
+            for (int l = 0; l < n; ++l) {
+                const u32 lo = (u32)__builtin_amdgcn_readlane((int)(u32)mine[b], l);
+                const u32 hi = (u32)__builtin_amdgcn_readlane((int)(u32)(mine[b] >> 32), l);
+                const u64 other = ((u64)hi << 32) | lo;
+#pragma unroll
+                for (int i = 0; i < ROUNDS; ++i) rank[i] += other < mine[i];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < ROUNDS; ++i)
+            if (i * 64 + lane < count && rank[i] < want) keys[rank[i]] = mine[i];
+        __builtin_amdgcn_wave_barrier();
+        if (count >= want) {
+            count = want;
+            limit = keys[want - 1];
+        }
+    }
+    // down to the `want` smallest, in no order: the want-th word bit by bit, among equal words the want-th index likewise
+    template <int ROUNDS> __device__ inline void cut_of(int lane)
+    {
+        u64 mine[ROUNDS];
+        u32 word[ROUNDS];
+#pragma unroll
+        for (int i = 0; i < ROUNDS; ++i) {
+            mine[i] = i * 64 + lane < count ? keys[i * 64 + lane] : ~0ULL;
+            word[i] = (u32)(mine[i] >> 32);
+        }
+        __builtin_amdgcn_wave_barrier();
+        int less, equal = 0;
+        const u32 w = wave_nth(word, want, less);
+#pragma unroll
+        for (int i = 0; i < ROUNDS; ++i) equal += __popcll(__ballot(word[i] == w));
+        u32 last = ~0u;
+        if (less + equal > want) {
+            u32 index[ROUNDS];
+#pragma unroll
+            for (int i = 0; i < ROUNDS; ++i) index[i] = word[i] == w ? (u32)mine[i] : ~0u;
+            int unused;
+            last = wave_nth(index, want - less, unused);
+        }
+        limit = ((u64)w << 32) | last;
+        count = 0;
+#pragma unroll
+        for (int i = 0; i < ROUNDS; ++i) {
+            const bool keep = mine[i] <= limit;
+            const u64 mask = __ballot(keep);
+            if (keep) keys[count + __popcll(mask & ((1ULL << lane) - 1))] = mine[i];
+            count += __popcll(mask);
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+    __device__ inline void cut(int lane)
+    {
+        __builtin_amdgcn_wave_barrier();
+        if (count <= 64) sort_of<1>(lane);
+        else if (count > want) {
+            if (count <= 256) cut_of<4>(lane);
+            else cut_of<(kListRoom + 192) / 64>(lane);
+        }
+    }
+    // (after a cut)
+    __device__ inline void sort(int lane)
+    {
+        __builtin_amdgcn_wave_barrier();
+        if (count <= 64) sort_of<1>(lane);
+        else sort_of<3>(lane);
+    }
+};
+
+// The list's `want` smallest of m keys (word(i), name(i)); a word of kOrderInf and more is nothing.
+template <class Word, class Name>
+__device__ inline void choose(KeyList &list, int m, int lane, Word word, Name name)
 {
-    constexpr int kThreads = 256;
+    for (int i0 = 0; i0 < m; i0 += 512) {
+        u32 v[8];
+#pragma unroll
+        for (int c = 0; c < 8; ++c) v[c] = i0 + c * 64 + lane < m ? word(i0 + c * 64 + lane) : ~0u;
+        u32 bound = ~0u;
+        if (list.limit == ~0ULL && m - i0 > list.want) {
+            // the want-th of the words, or of the lanes' smallest words: at least want of the words do not exceed either, and
+            // where want is far below 64 few more do
+            int unused;
+            if (list.want <= 32) {
+                u32 low[1] = {v[0]};
+#pragma unroll
+                for (int c = 1; c < 8; ++c) low[0] = min(low[0], v[c]);
+                bound = wave_nth(low, list.want, unused);
+            } else bound = wave_nth(v, list.want, unused);
+        }
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+            const bool take = v[c] < kOrderInf && v[c] <= bound;
+            if (__any(take)) list.push(((u64)v[c] << 32) | (u32)(take ? name(i0 + c * 64 + lane) : 0), take, lane);
+        }
+        list.cut(lane);
+    }
+}
+
+// u of the 16 rows from row0 (the same for all lanes) on: start values, then products of S steps whose operands are
+// loaded together, TILES tiles side by side.  row0 is a row of the table; rows past its end have u = inf.
+template <int S, int TILES>
+__device__ inline void score_tiles(const Table &t, const Table &q, const Operand &first, int qrow, int r, int g, const int (&row0)[TILES],
+                                   f32x4 (&acc)[TILES])
+{
+    const int steps = (t.nb + 3) / 4;
+    int row[TILES];
+    bool ok[TILES], odd = false;
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) {
+        const int left = t.n - row0[i];
+        row[i] = min(r, left - 1);
+        // (as few loads as there can be: what returns them is busy 9 cycles of 10 where many queries pick)
+        acc[i] = f32x4{__builtin_inff(), 0.0f, 0.0f, 0.0f};
+        if (left >= 16) acc[i] = *(const f32x4 *)(t.norms + row0[i] + 4 * g);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) odd |= !mx_takes_part(acc[i][c]);
+        ok[i] = true;
+    }
+    if (__any(odd)) {
+#pragma unroll
+        for (int i = 0; i < TILES; ++i) {
+            const int left = t.n - row0[i];
+            const float *norms = t.norms + row0[i];
+            const auto start = [&](int c) {
+                const float norm = norms[min(4 * g + c, left - 1)];
+                return 4 * g + c < left && mx_takes_part(norm) ? norm : __builtin_inff();
+            };
+            ok[i] = mx_takes_part(norms[row[i]]);
+            acc[i] = f32x4{start(0), start(1), start(2), start(3)};
+        }
+    }
+    for (int s0 = 0; s0 < steps; s0 += S) {
+        Operand y[S], x[S][TILES];
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            const int block = 4 * (s0 + s) + g;
+            y[s] = S == 1 && s0 == 0 ? first : mx_query(q, qrow, block, true);
+#pragma unroll
+            for (int i = 0; i < TILES; ++i) {
+                const uint8_t *codes = t.codes + (size_t)row0[i] * t.nb * 16, *scales = t.scales + (size_t)row0[i] * t.sp;
+                x[s][i] = {{0, 0, 0, 0}, 0};
+                if (block < t.nb) {
+                    x[s][i].codes = *(const i32x4 *)(codes + (u32)(__umul24(row[i], t.nb) + block) * 16);
+                    x[s][i].scale = scales[(u32)(__umul24(row[i], t.sp) + block)];
+                }
+            }
+        }
+#pragma unroll
+        for (int s = 0; s < S; ++s)
+#pragma unroll
+            for (int i = 0; i < TILES; ++i) {
+                if (!ok[i]) x[s][i].scale = 0;
+                acc[i] = mx_mma(x[s][i], y[s], acc[i]);
+            }
+    }
+}
+
+// WAVES waves per query (one: many queries; several: few).  All of them choose the same supers and groups; the rows of
+// the groups are shared out, and the waves' lists meet in the first one's.
+template <int WAVES, int S>
+__global__ __launch_bounds__(64 * WAVES) void pick_kernel(Scan a, int k, long long first_self, int *ids, float *dists)
+{
     extern __shared__ u64 lds[];
-    __shared__ PickShared sh;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int qi = blockIdx.x, kk = k + (first_self >= 0 ? 1 : 0), group = 4 * a.tiles;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
+    // sixteen neighbouring queries, whose minima lie side by side, on one chiplet (every eighth workgroup)
+    const int qi = WAVES > 1 ? blockIdx.x : (blockIdx.x & ~127) + (blockIdx.x & 7) * 16 + ((blockIdx.x >> 3) & 15);
+    if (qi >= a.nq) return;
+    const int kk = k + (first_self >= 0 ? 1 : 0), group = 4 * a.tiles;
     const Table &t = a.t, &q = a.q;
     const int self = first_self >= 0 ? (int)min(first_self + a.first + qi, 0x7FFFFFFFLL) : -1;
-    int key_slots = 1;
-    while (key_slots < kk * group) key_slots <<= 1;
-    u64 *keys = lds;
-    u32 *values = (u32 *)(keys + key_slots);
-    int *chosen_supers = (int *)(values + 16 * kk);
-    int *chosen = chosen_supers + kk;
+    u64 *mine = lds + wave * (2 * kk + kListRoom);
+    u64 *chosen = mine + kk + kListRoom;
     int *out_ids = ids + (size_t)(a.first + qi) * k;
     float *out_dists = dists + (size_t)(a.first + qi) * k;
     const float qnorm = q.norms[a.first + qi];
-    int found = 0;
+    KeyList list;
+    list.start(mine, kk);
     if (mx_takes_part(qnorm) && t.n > 0) {
         const float *sm = a.smin + ((size_t)(qi >> 4) * a.supers) * 16 + (qi & 15);
         const float *gm = a.gmin + ((size_t)(qi >> 4) * a.supers * 16) * 16 + (qi & 15);
-        int n_supers, n_groups;
-        choose<kThreads>([&](int i) { return mx_order(sm[(size_t)i * 16]); }, a.supers, kk, chosen_supers, sh, n_supers);
-        for (int i = tid; i < n_supers * 16; i += kThreads)
-            values[i] = mx_order(gm[((size_t)chosen_supers[i >> 4] * 16 + (i & 15)) * 16]);
-        __syncthreads();
-        const u32 limit = choose<kThreads>([&](int i) { return values[i]; }, n_supers * 16, kk, chosen, sh, n_groups);
-        if (tid == 0) sh.count = 0;
-        __syncthreads();
-        // values of the chosen groups' rows; every column of the instruction holds the query
-        const int r = lane & 15, g = lane >> 4, per_group = (group + 15) / 16;
-        for (int tile = wave; tile < n_groups * per_group; tile += kThreads / 64) {
-            const int c = chosen[tile / per_group];
-            const int row0 = (chosen_supers[c >> 4] * 16 + (c & 15)) * group + (tile % per_group) * 16;
-            f32x4 acc;
+        choose(list, a.supers, lane, [&](int i) { return mx_order(sm[(size_t)i * 16]); }, [&](int i) { return i; });
+        const int n_supers = list.count;
+        for (int i = lane; i < n_supers; i += 64) chosen[i] = mine[i];
+        __builtin_amdgcn_wave_barrier();
+        list.start(mine, kk);
+        const auto group_of = [&](int i) { return (int)(u32)chosen[i >> 4] * 16 + (i & 15); };
+        choose(list, n_supers * 16, lane, [&](int i) { return mx_order(gm[(size_t)group_of(i) * 16]); }, group_of);
+        const int n_groups = list.count;
+        const u32 bound = (u32)(list.limit >> 32);
+        __builtin_amdgcn_wave_barrier();
+        for (int i = lane; i < n_groups; i += 64) chosen[i] = mine[i];
+        __builtin_amdgcn_wave_barrier();
+        list.start(mine, kk);
+        // values of the groups' rows, four tiles of 16 at a time; every column of the instruction holds the query, and lane
+        // (g, r < 4) looks after row 4 g + r of a tile
+        const Operand first = mx_query(q, a.first + qi, g, true);
+        const float farthest = bound < kOrderInf ? mx_unorder(bound) : 3.402823466e+38f;
+        const int per_group = group / 16, log_per_group = 31 - __clz(per_group), n_tiles = n_groups << log_per_group;
+        for (int tile0 = wave * 4; tile0 < n_tiles; tile0 += WAVES * 4) {
+            int row0[4];
+            bool live[4];
+            f32x4 acc[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int x = row0 + 4 * g + j;
-                const float norm = x < t.n ? t.norms[x] : __builtin_inff();
-                acc[j] = mx_takes_part(norm) ? norm : __builtin_inff();
+            for (int i = 0; i < 4; ++i) {
+                const int tile = min(tile0 + i, n_tiles - 1);
+                const int id = __builtin_amdgcn_readfirstlane((int)(u32)chosen[tile >> log_per_group]);
+                row0[i] = id * group + (tile & (per_group - 1)) * 16;
+                live[i] = tile0 + i < n_tiles && row0[i] < t.n;      // (the table can end inside a group)
+                row0[i] = live[i] ? row0[i] : 0;
             }
-            const int row = min(row0 + r, t.n - 1);
-            const bool ok = mx_takes_part(t.norms[row]);
-            for (int s = 0; s < (t.nb + 3) / 4; ++s) {
-                Operand x = mx_load(t, row, 4 * s + g);
-                if (!ok) x.scale = 0;
-                acc = mx_mma(x, mx_query(q, a.first + qi, 4 * s + g, true), acc);
+            score_tiles<S, 4>(t, q, first, a.first + qi, r, g, row0, acc);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float u = r == 0 ? acc[i][0] : r == 1 ? acc[i][1] : r == 2 ? acc[i][2] : acc[i][3];
+                const int id = row0[i] + 4 * g + r;
+                const bool take = r < 4 && u <= farthest && id != self && live[i];
+                if (__any(take)) list.push(((u64)mx_order(u) << 32) | (u32)id, take, lane);
             }
-            const float u = r == 0 ? acc[0] : r == 1 ? acc[1] : r == 2 ? acc[2] : acc[3];
-            const int id = row0 + 4 * g + r;
-            const u32 order = mx_order(u);
-            if (r < 4 && id < t.n && id != self && order < kOrderInf && order <= limit)
-                keys[atomicAdd(&sh.count, 1u)] = ((u64)order << 32) | (u32)id;
+            if (list.count > kListRoom - 64) list.cut(lane);
         }
-        __syncthreads();
-        found = (int)sh.count;
+        list.cut(lane);
     }
-    int pow2 = 1;
-    while (pow2 < found) pow2 <<= 1;
-    for (int i = found + tid; i < pow2; i += kThreads) keys[i] = ~0ULL;
-    __syncthreads();
-    for (int size = 2; size <= pow2; size <<= 1)
-        for (int step = size >> 1; step > 0; step >>= 1) {
-            for (int i = tid; i < pow2 / 2; i += kThreads) {
-                const int lo = 2 * step * (i / step) + i % step, hi = lo + step;
-                const u64 x = keys[lo], y = keys[hi];
-                if ((x > y) == ((lo & size) == 0)) {
-                    keys[lo] = y;
-                    keys[hi] = x;
-                }
-            }
-            __syncthreads();
+    if (WAVES > 1) {
+        __shared__ int counts[WAVES];
+        if (lane == 0) counts[wave] = list.count;
+        __syncthreads();
+        if (wave != 0) return;
+        for (int w = 1; w < WAVES; ++w) {
+            const u64 *theirs = lds + w * (2 * kk + kListRoom);
+            const int c = counts[w];
+            for (int i0 = 0; i0 < c; i0 += 64) list.push(i0 + lane < c ? theirs[i0 + lane] : 0, i0 + lane < c, lane);
+            if (list.count > kListRoom - 256 || w == WAVES - 1) list.cut(lane);
         }
-    for (int i = tid; i < k; i += kThreads) {
-        const bool live = i < found;
-        const float u = live ? mx_unorder((u32)(keys[i] >> 32)) : 0.0f;
-        out_ids[i] = live ? (int)(u32)keys[i] : -1;
-        out_dists[i] = live ? fmaxf(qnorm + u, 0.0f) : __builtin_inff();
+    }
+    list.sort(lane);
+    for (int i = lane; i < k; i += 64) {
+        const bool live = i < list.count;
+        const u64 key = live ? mine[i] : 0;
+        out_ids[i] = live ? (int)(u32)key : -1;
+        out_dists[i] = live ? fmaxf(qnorm + mx_unorder((u32)(key >> 32)), 0.0f) : __builtin_inff();
     }
 }
 
 struct NearestShape {
     int tiles, supers, chunk;      // tiles per block, supers of the table, queries per pass
-    size_t gmin_bytes, bytes, lds;
+    size_t gmin_bytes, bytes;
 };
 inline NearestShape nearest_shape(int64_t n, int64_t nq, int k)
 {
     NearestShape s;
     // Group size: the scan writes a value per group, the pick reads the rows of k groups.
     s.tiles = 4;
-    while (s.tiles < 16 && (int64_t)s.tiles * s.tiles * 4 * 300 * (k + 1) <= n && (k + 1) * 4 * s.tiles * 2 <= 8192) s.tiles *= 2;
+    while (s.tiles < 16 && (int64_t)s.tiles * s.tiles * 4 * 300 * (k + 1) <= n) s.tiles *= 2;
     const int64_t super_rows = 64 * s.tiles;
     s.supers = (int)((n + super_rows - 1) / super_rows);
     const size_t per16 = (size_t)s.supers * 17 * 16 * sizeof(float);     // 16 queries: groups and supers
@@ -749,11 +871,24 @@ inline NearestShape nearest_shape(int64_t n, int64_t nq, int k)
     s.chunk = (int)(sixteens * 16);
     s.gmin_bytes = align_up(sixteens * s.supers * 16 * 16 * sizeof(float));
     s.bytes = s.gmin_bytes + align_up(sixteens * s.supers * 16 * sizeof(float)) + 256;
-    const int kk = k + 1;
-    size_t slots = 1;
-    while (slots < (size_t)kk * 4 * s.tiles) slots <<= 1;
-    s.lds = slots * 8 + (size_t)kk * 16 * 4 + (size_t)kk * 8;
     return s;
+}
+
+template <int WAVES, int S>
+int launch_pick_of(const Scan &a, int k, int64_t first_self, int32_t *ids, float *dists, hipStream_t st)
+{
+    const int kk = k + (first_self >= 0 ? 1 : 0), lds = WAVES * (2 * kk + kListRoom) * 8;
+    EF_HIP_CHECK(hipFuncSetAttribute((const void *)pick_kernel<WAVES, S>, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+    const int blocks = WAVES > 1 ? a.nq : (a.nq + 127) & ~127;
+    pick_kernel<WAVES, S><<<(unsigned)blocks, 64 * WAVES, lds, st>>>(a, k, first_self, ids, dists);
+    return EFANNA_OK;
+}
+template <int S>
+int launch_pick(const Scan &a, int k, int64_t first_self, int32_t *ids, float *dists, hipStream_t st)
+{
+    if (a.nq > 2048) return launch_pick_of<1, S>(a, k, first_self, ids, dists, st);
+    if (a.nq > 256) return launch_pick_of<4, S>(a, k, first_self, ids, dists, st);
+    return launch_pick_of<8, S>(a, k, first_self, ids, dists, st);
 }
 
 template <int KS, int QF>
@@ -762,8 +897,11 @@ int launch_wide(Scan a, hipStream_t st)
     const int lds = 2 * (int)sizeof(StageLds<KS>);
     EF_HIP_CHECK(hipFuncSetAttribute((const void *)scan_wide_kernel<KS, QF>, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
     a.q_parts = (a.nq + 128 * QF - 1) / (128 * QF);
-    const int tiles = 256;                                // per workgroup, about
-    a.per_wg = tiles / (4 * a.tiles) > 1 ? tiles / (4 * a.tiles) : 1;
+    // supers per workgroup: enough for its queries' loads to be little next to its rows', few enough to fill the CUs (two workgroups
+    // of one step each, one of more) twice
+    const int64_t share = (int64_t)a.supers * a.q_parts / (KS == 1 ? 1024 : 512), most = 256 / (4 * a.tiles), least = 32 / (4 * a.tiles);
+    a.per_wg = (int)(share > most ? most : share < least ? least : share);
+    if (a.per_wg < 1) a.per_wg = 1;
     const int64_t slices = (a.supers + a.per_wg - 1) / a.per_wg;
     const int64_t grid = (slices + 7) / 8 * 8 * a.q_parts;
     if (grid > 2147483647LL) return EFANNA_EUNSUPPORTED;
@@ -897,7 +1035,6 @@ extern "C" int efanna_mx_nearest(const uint8_t *codes, const uint8_t *scales, co
     const int nb = mx_blocks(d), sp = mx_scale_pitch(d);
     const Table t = {codes, scales, norms, (int)n, nb, sp}, q = {q_codes, q_scales, q_norms, (int)nq, nb, sp};
     Scan a = {t, q, 0, 0, sh.tiles, sh.supers, 0, 0, (float *)ws, (float *)((char *)ws + sh.gmin_bytes)};
-    EF_HIP_CHECK(hipFuncSetAttribute((const void *)pick_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)sh.lds));
     for (int64_t first = 0; first < nq; first += sh.chunk) {
         a.first = (int)first;
         a.nq = (int)(nq - first < sh.chunk ? nq - first : sh.chunk);
@@ -906,7 +1043,8 @@ extern "C" int efanna_mx_nearest(const uint8_t *codes, const uint8_t *scales, co
             if (rc != EFANNA_OK) return rc;
             EF_HIP_CHECK(hipGetLastError());
         }
-        pick_kernel<<<(unsigned)a.nq, 256, sh.lds, st>>>(a, k, first_self, ids, dists);
+        const int rc = a.t.nb <= 4 ? launch_pick<1>(a, k, first_self, ids, dists, st) : launch_pick<4>(a, k, first_self, ids, dists, st);
+        if (rc != EFANNA_OK) return rc;
         EF_HIP_CHECK(hipGetLastError());
     }
     return EFANNA_OK;

@@ -332,6 +332,20 @@ def test_nearest(ef, kind, n, nq, d, k):
     check_nearest(ef.efanna_mx_nearest(t, q, k), X, Q, k)
 
 
+@pytest.mark.parametrize("n,k", [(160_001, 1), (160_017, 1), (160_063, 1), (38_401, 1), (38_417, 1), (250_049, 2)])
+@pytest.mark.parametrize("nq", [3, 130])
+def test_nearest_where_the_table_ends_inside_a_group(ef, n, k, nq):
+    """Large tables are taken in groups of 32 and 64 rows; the last rows are among the answers."""
+    rng = np.random.default_rng(n)
+    x = vectors(rng, n, 16, "grid") + np.float32(9.0)
+    x[-70:] = vectors(rng, 70, 16, "grid")
+    t, X = table(ef, x)
+    q, Q = table(ef, vectors(rng, nq, 16, "grid"))
+    got = ef.efanna_mx_nearest(t, q, k)
+    check_nearest(got, X, Q, k)
+    assert (host(got[0]) >= n - 70).all()
+
+
 @pytest.mark.parametrize("n,d,k,first", [(300, 24, 5, 0), (2000, 64, 30, 0), (2000, 64, 128, 1990), (1, 8, 2, 0), (500, 8, 4, 200)])
 def test_nearest_of_own_rows_leaves_each_out(ef, n, d, k, first):
     rng = np.random.default_rng(n + first)
