@@ -196,6 +196,9 @@ __global__ __launch_bounds__(256) void product_kernel(Table a, Table b, T *out, 
 // Four groups are passed over together ("block"): tile t of `tiles` holds as instruction row r the block's row
 // (r / 4) * 4 tiles + 4 t + r % 4, so that the four values of a lane belong to one group in every tile and its
 // running minimum needs no other lane.  A group is 4 tiles rows, a super four blocks.
+typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((address_space(1))) const void global_void;
+
 constexpr float kNormLimit = 8.507059173023462e37f;      // 2^126
 __device__ inline bool mx_takes_part(float norm) { return norm < kNormLimit; }
 __device__ inline float mx_min(float a, float b) { return __builtin_elementwise_minimum(a, b); }
@@ -337,26 +340,91 @@ struct Queries {
     }
 };
 
-typedef __attribute__((address_space(3))) void lds_void;
-typedef __attribute__((address_space(1))) const void global_void;
+
+// Rows pass through LDS by loads that write there directly.  An operand (16 rows, a step's 4 blocks) is 1 KiB; lane l of
+// its load brings a 16-byte block of row l / 4, so that four lanes share 64 consecutive bytes of memory (with the lanes in the
+// order the matrix instruction wants them the loads return a quarter as fast).  The blocks of row r lie in the order
+// b ^ (r / 4), so that the 16 rows' blocks b, which are read together, are in different banks.
+__device__ inline int mx_stage_block(int lane, int step, int nb) { return min(4 * step + ((lane & 3) ^ (lane >> 4)), nb - 1); }
+__device__ inline int mx_staged_at(int r, int g) { return (r * 4 + (g ^ (r >> 2))) * 4; }      // word within the operand
+__device__ inline void mx_stage(const void *from, void *to, int lane_bytes_16)
+{
+    if (lane_bytes_16) __builtin_amdgcn_global_load_lds((global_void *)from, (lds_void *)to, 16, 0, 0);
+    else __builtin_amdgcn_global_load_lds((global_void *)from, (lds_void *)to, 4, 0, 0);
+}
+
+template <int TILES, int KS>
+struct StageLds {
+    static constexpr int tiles = TILES, ops = TILES * KS;
+    u32 codes[ops][256];
+    u32 scales[(ops + 3) / 4 * 4][16];       // [tile * KS + s][row]: the scales of the row's blocks 4 s .. 4 s + 3
+    float norms[(TILES + 3) / 4 * 4][16];
+    // The waves' share of loading: row_of(tile, r) is row r of a tile of the stage, and exists.
+    template <int WAVES, class RowOf> __device__ inline void load(const Table &t, int wave, int lane, RowOf row_of)
+    {
+        const int r = lane & 15, g = lane >> 4;
+#pragma unroll
+        for (int i = 0; i < (ops + WAVES - 1) / WAVES; ++i) {
+            const int op = wave + WAVES * i;
+            if (WAVES * (i + 1) <= ops || op < ops)
+                mx_stage(t.codes + ((size_t)row_of(op / KS, lane >> 2) * t.nb + mx_stage_block(lane, op % KS, t.nb)) * 16,
+                         &codes[op][0], 1);
+        }
+#pragma unroll
+        for (int i = 0; i < ((ops + 3) / 4 + WAVES - 1) / WAVES; ++i) {
+            const int op = (wave + WAVES * i) * 4 + g;
+            if (op < ops) mx_stage(t.scales + (size_t)row_of(op / KS, r) * t.sp + 4 * (op % KS), &scales[(wave + WAVES * i) * 4][0], 0);
+        }
+#pragma unroll
+        for (int i = 0; i < ((TILES + 3) / 4 + WAVES - 1) / WAVES; ++i) {
+            const int tile = (wave + WAVES * i) * 4 + g;
+            if (tile < TILES) mx_stage(t.norms + row_of(tile, r), &norms[(wave + WAVES * i) * 4][0], 0);
+        }
+    }
+    // whether a row of the stage does not take part
+    __device__ inline bool odd(int lane) const
+    {
+        bool any = false;
+#pragma unroll
+        for (int i = 0; i < (TILES * 16 + 63) / 64; ++i)
+            if (i * 64 + lane < TILES * 16) any |= !mx_takes_part((&norms[0][0])[i * 64 + lane]);
+        return __any(any);
+    }
+};
+// A tile of a stage as an operand for Queries::tile.  b, b_last: the lane's block in a step and in the last one, where the
+// place of missing blocks is taken by the row's last (the queries' zeros there count).
+template <class Lds, int KS>
+struct StagedRows {
+    const Lds *l;
+    int tile, r, at, b, b_last;
+    bool out;
+    __device__ i32x4 codes(int s) const { return *(const i32x4 *)&l->codes[tile * KS + s][at]; }
+    __device__ int scale(int s) const
+    {
+        const int v = ((const uint8_t *)&l->scales[tile * KS + s][r])[s < KS - 1 ? b : b_last];
+        return out ? 0 : v;
+    }
+};
+// Start values of the tile's rows 4 g .. 4 g + 3; CAREFUL: rows from `left` on do not exist, rows out of range do not take part.
+template <bool CAREFUL, class Lds>
+__device__ inline f32x4 mx_start(const Lds *l, int tile, int g, int left)
+{
+    f32x4 start = *(const f32x4 *)&l->norms[tile][4 * g];
+    if (CAREFUL)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) start[c] = c < left && mx_takes_part(start[c]) ? start[c] : __builtin_inff();
+    return start;
+}
 
 // Many queries: a workgroup of 8 waves holds 8 * QF * 16 queries in registers and passes the rows of its supers
-// through LDS, a stage of kStage operands at a time, asynchronously loaded while the stage before is computed.
-// An operand lies in LDS as the lanes read it (lane * 16 bytes), its rows gathered by the loading lanes' addresses.
+// through LDS, a stage of about kStage operands at a time, loaded while the stage before is computed.
 constexpr int kStage = 32;
-template <int KS>
-struct StageLds {
-    static constexpr int tiles = KS == 1 ? kStage : KS == 2 ? kStage / 2 : KS <= 4 ? kStage / 4 : kStage / 8;      // (a power of two)
-    u32 codes[tiles * KS][256];
-    u32 scales[(tiles * KS + 3) / 4 * 4][16];      // [tile * KS + s][row]: the scales of the row's blocks 4 s .. 4 s + 3
-    float norms[tiles][16];
-};
 
 template <int KS, int QF>
 __global__ __launch_bounds__(512, KS == 1 ? 4 : 2) void scan_wide_kernel(Scan a)
 {
-    typedef StageLds<KS> Lds;
-    constexpr int TS = Lds::tiles, kOps = TS * KS;
+    constexpr int TS = KS == 1 ? kStage : KS == 2 ? kStage / 2 : KS <= 4 ? kStage / 4 : kStage / 8;      // (a power of two)
+    typedef StageLds<TS, KS> Lds;
     extern __shared__ __align__(16) char lds_raw[];
     Lds *stage = (Lds *)lds_raw;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
@@ -370,41 +438,12 @@ __global__ __launch_bounds__(512, KS == 1 ? 4 : 2) void scan_wide_kernel(Scan a)
     q.load(a, q0, r, g);
     const int tile_lo = s0 * 4 * a.tiles, tile_hi = s1 * 4 * a.tiles;      // tiles counted through the table
     const int log_tiles = 31 - __clz(a.tiles), run = min(TS, a.tiles);
+    const int at_lane = mx_staged_at(r, g), b_last = min(4 * (KS - 1) + g, a.t.nb - 1) & 3;
     const auto row_of = [&](int tile, int row) {
         return mx_tile_row((tile >> log_tiles) * 16 * a.tiles, a.tiles, tile & (a.tiles - 1), row);
     };
     const auto load = [&](int buffer, int tile0) {
-        Lds *to = stage + buffer;
-#pragma unroll
-        for (int i = 0; i < (kOps + 7) / 8; ++i) {
-            const int op = wave + 8 * i;
-            if (op < kOps) {
-                const int s = op % KS, row = min(row_of(tile0 + op / KS, r), a.t.n - 1);
-                const uint8_t *p = a.t.codes + ((size_t)row * a.t.nb + min(4 * s + g, a.t.nb - 1)) * 16;
-                __builtin_amdgcn_global_load_lds((global_void *)p, (lds_void *)&to->codes[op][0], 16, 0, 0);
-            }
-        }
-        constexpr int kScaleLoads = (kOps + 3) / 4;         // 64 words each
-#pragma unroll
-        for (int i = 0; i < (kScaleLoads + 7) / 8; ++i) {
-            const int part4 = wave + 8 * i;
-            if (part4 < kScaleLoads) {
-                const int op = part4 * 4 + g;
-                if (op < kOps) {
-                    const int row = min(row_of(tile0 + op / KS, r), a.t.n - 1);
-                    const uint8_t *p = a.t.scales + (size_t)row * a.t.sp + 4 * (op % KS);
-                    __builtin_amdgcn_global_load_lds((global_void *)p, (lds_void *)&to->scales[part4 * 4][0], 4, 0, 0);
-                }
-            }
-        }
-        constexpr int kNormLoads = (TS * 16 + 63) / 64;
-        if (wave < kNormLoads) {
-            const int tile = wave * 4 + g;
-            if (tile < TS) {
-                const float *p = a.t.norms + min(row_of(tile0 + tile, r), a.t.n - 1);
-                __builtin_amdgcn_global_load_lds((global_void *)p, (lds_void *)&to->norms[wave * 4][0], 4, 0, 0);
-            }
-        }
+        stage[buffer].template load<8>(a.t, wave, lane, [&](int tile, int row) { return min(row_of(tile0 + tile, row), a.t.n - 1); });
     };
     const auto arrived = [&]() {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -419,44 +458,25 @@ __global__ __launch_bounds__(512, KS == 1 ? 4 : 2) void scan_wide_kernel(Scan a)
         if (tile0 + TS < tile_hi) load(buffer ^ 1, tile0 + TS);
         const Lds *from = stage + buffer;
         // rows that do not take part, or do not exist, anywhere in the stage?
-        bool odd = row_of(min(tile0 + TS, tile_hi) - 1, 15) >= a.t.n;
-#pragma unroll
-        for (int i = 0; i < (TS * 16 + 63) / 64; ++i)
-            if (i * 64 + lane < TS * 16) odd |= !mx_takes_part((&from->norms[0][0])[i * 64 + lane]);
-        const bool careful = __any(odd);
-        struct Rows {
-            const Lds *l;
-            int tile, lane, r, b, b_last;
-            bool out;
-            __device__ i32x4 codes(int s) const { return *(const i32x4 *)&l->codes[tile * KS + s][lane * 4]; }
-            __device__ int scale(int s) const
-            {
-                const int v = ((const uint8_t *)&l->scales[tile * KS + s][r])[s < KS - 1 ? b : b_last];
-                return out ? 0 : v;
-            }
-        };
-        // (the last step's missing blocks: the scale of the block whose codes were loaded in their place)
-        const int b_last = min(4 * (KS - 1) + g, a.t.nb - 1) & 3;
+        const bool careful = from->odd(lane) || row_of(min(tile0 + TS, tile_hi) - 1, 15) >= a.t.n;
         const auto pass = [&](auto careful_, int first_tile) {
-#pragma unroll 4
-            for (int i = 0; i < run; ++i) {
-                const int tile = first_tile + i;
-                f32x4 start = *(const f32x4 *)&from->norms[tile][4 * g];
-                Rows x = {from, tile, lane, r, g, b_last, false};
-                if constexpr (decltype(careful_)::value) {
-                    x.out = !mx_takes_part(from->norms[tile][r]);
+            constexpr bool kCareful = decltype(careful_)::value;
+            constexpr int kTogether = kCareful || KS > 2 ? 1 : 2;
+            for (int i0 = 0; i0 < run; i0 += kTogether)
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
-                        if (row_of(tile0 + tile, 4 * g + c) >= a.t.n || !mx_takes_part(start[c])) start[c] = __builtin_inff();
-                }
-                f32x4 acc[QF];
-                q.tile(x, start, acc);
+                for (int i = 0; i < kTogether; ++i) {
+                    const int tile = first_tile + i0 + i;
+                    const f32x4 start = mx_start<kCareful>(from, tile, g, a.t.n - row_of(tile0 + tile, 4 * g));
+                    StagedRows<Lds, KS> x = {from, tile, r, at_lane, g, b_last, false};
+                    if (kCareful) x.out = !mx_takes_part(from->norms[tile][r]);
+                    f32x4 acc[QF];
+                    q.tile(x, start, acc);
 #pragma unroll
-                for (int f = 0; f < QF; ++f) {
-                    best[f] = mx_min(mx_min(best[f], acc[f][0]), acc[f][1]);
-                    best[f] = mx_min(mx_min(best[f], acc[f][2]), acc[f][3]);
+                    for (int f = 0; f < QF; ++f) {
+                        best[f] = mx_min(mx_min(best[f], acc[f][0]), acc[f][1]);
+                        best[f] = mx_min(mx_min(best[f], acc[f][2]), acc[f][3]);
+                    }
                 }
-            }
         };
         const int n_tiles = min(TS, tile_hi - tile0);
         for (int tile = 0; tile < n_tiles; tile += run) {
@@ -485,59 +505,51 @@ __global__ __launch_bounds__(512, KS == 1 ? 4 : 2) void scan_wide_kernel(Scan a)
     }
 }
 
-// Few queries: all four waves of a workgroup hold the same QF * 16 of them and take a block of a super each.  The rows
-// are read once, straight into registers, many tiles ahead: bound by HBM.
+// Few queries: all four waves of a workgroup hold the same QF * 16 of them and take a block of a super each, up to 16
+// operands of it in flight.  Bound by HBM: the rows are read once.
 template <int KS, int QF>
-__global__ __launch_bounds__(256) void scan_narrow_kernel(Scan a)
+__global__ __launch_bounds__(256, 2) void scan_narrow_kernel(Scan a)
 {
+    constexpr int TS = KS == 1 ? 16 : KS == 2 ? 8 : KS <= 4 ? 4 : 2;
+    typedef StageLds<TS, KS> Lds;
+    extern __shared__ __align__(16) char lds_raw[];
     __shared__ float share[4][QF][16];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
     const int super = blockIdx.x, q0 = blockIdx.y * QF * 16;
-    Queries<KS, QF> q;
-    q.load(a, q0, r, g);
     const int row0 = (super * 4 + wave) * 16 * a.tiles;
+    Lds *stage = (Lds *)lds_raw + wave;
+    const int at_lane = mx_staged_at(r, g), b_last = min(4 * (KS - 1) + g, a.t.nb - 1) & 3;
+    Queries<KS, QF> q;
     float best[QF];
 #pragma unroll
     for (int f = 0; f < QF; ++f) best[f] = __builtin_inff();
-    constexpr int kAhead = KS >= 3 ? 1 : 4 / KS;              // tiles loaded together
-    struct Rows {
-        i32x4 c[KS];
-        int sc[KS];
-        __device__ i32x4 codes(int s) const { return c[s]; }
-        __device__ int scale(int s) const { return sc[s]; }
-    };
-    for (int tile0 = 0; tile0 < a.tiles; tile0 += kAhead) {
-        Rows x[kAhead];
-        f32x4 start[kAhead];
+    for (int tile0 = 0; tile0 < a.tiles; tile0 += TS) {
+        // (tiles past the block's end are its last one again)
+        const auto row_of = [&](int tile, int row) {
+            return min(mx_tile_row(row0, a.tiles, min(tile0 + tile, a.tiles - 1), row), a.t.n - 1);
+        };
+        stage->template load<1>(a.t, 0, lane, row_of);
+        if (tile0 == 0) q.load(a, q0, r, g);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        const auto pass = [&](auto careful_) {
+            constexpr bool kCareful = decltype(careful_)::value;
+#pragma unroll(kCareful ? 1 : KS <= 2 ? 4 : 1)
+            for (int tile = 0; tile < TS; ++tile) {
+                const int left = a.t.n - mx_tile_row(row0, a.tiles, min(tile0 + tile, a.tiles - 1), 4 * g);
+                const f32x4 start = mx_start<kCareful>(stage, tile, g, left);
+                StagedRows<Lds, KS> x = {stage, tile, r, at_lane, g, b_last, false};
+                if (kCareful) x.out = !mx_takes_part(stage->norms[tile][r]);
+                f32x4 acc[QF];
+                q.tile(x, start, acc);
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const int tile = min(tile0 + i, a.tiles - 1);
-            const int row = min(mx_tile_row(row0, a.tiles, tile, r), a.t.n - 1);
-#pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                const int block = min(4 * s + g, a.t.nb - 1);
-                x[i].c[s] = *(const i32x4 *)(a.t.codes + ((size_t)row * a.t.nb + block) * 16);
-                x[i].sc[s] = a.t.scales[(size_t)row * a.t.sp + block];
+                for (int f = 0; f < QF; ++f) {
+                    best[f] = mx_min(mx_min(best[f], acc[f][0]), acc[f][1]);
+                    best[f] = mx_min(mx_min(best[f], acc[f][2]), acc[f][3]);
+                }
             }
-            const bool ok = mx_takes_part(a.t.norms[row]);
-#pragma unroll
-            for (int s = 0; s < KS; ++s) x[i].sc[s] = ok ? x[i].sc[s] : 0;
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const int y = mx_tile_row(row0, a.tiles, tile, 4 * g + c);
-                const float norm = y < a.t.n ? a.t.norms[y] : __builtin_inff();
-                start[i][c] = mx_takes_part(norm) ? norm : __builtin_inff();
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            f32x4 acc[QF];
-            q.tile(x[i], start[i], acc);
-#pragma unroll
-            for (int f = 0; f < QF; ++f)
-#pragma unroll
-                for (int c = 0; c < 4; ++c) best[f] = mx_min(best[f], acc[f][c]);
-        }
+        };
+        if (stage->odd(lane) || row0 + 16 * a.tiles > a.t.n) pass(std::true_type());
+        else pass(std::false_type());
     }
 #pragma unroll
     for (int f = 0; f < QF; ++f) {
@@ -616,10 +628,7 @@ struct KeyList {
         for (int i = 0; i < ROUNDS; ++i)
             if (i * 64 + lane < count && rank[i] < want) keys[rank[i]] = mine[i];
         __builtin_amdgcn_wave_barrier();
-        if (count >= want) {
-            count = want;
-            limit = keys[want - 1];
-        }
+        count = min(count, want);
     }
     // down to the `want` smallest, in no order: the want-th word bit by bit, among equal words the want-th index likewise
     template <int ROUNDS> __device__ inline void cut_of(int lane)
@@ -658,15 +667,14 @@ struct KeyList {
     __device__ inline void cut(int lane)
     {
         __builtin_amdgcn_wave_barrier();
-        if (count <= 64) sort_of<1>(lane);
-        else if (count > want) {
-            if (count <= 256) cut_of<4>(lane);
-            else cut_of<(kListRoom + 192) / 64>(lane);
-        }
+        if (count < want) return;
+        if (count <= 64) cut_of<1>(lane);
+        else if (count <= 256) cut_of<4>(lane);
+        else cut_of<(kListRoom + 192) / 64>(lane);
     }
-    // (after a cut)
     __device__ inline void sort(int lane)
     {
+        if (count > 192) cut(lane);
         __builtin_amdgcn_wave_barrier();
         if (count <= 64) sort_of<1>(lane);
         else sort_of<3>(lane);
@@ -680,7 +688,9 @@ __device__ inline void choose(KeyList &list, int m, int lane, Word word, Name na
     for (int i0 = 0; i0 < m; i0 += 512) {
         u32 v[8];
 #pragma unroll
-        for (int c = 0; c < 8; ++c) v[c] = i0 + c * 64 + lane < m ? word(i0 + c * 64 + lane) : ~0u;
+        for (int c = 0; c < 8; ++c) v[c] = word(min(i0 + c * 64 + lane, m - 1));      // (no load waits behind a condition)
+#pragma unroll
+        for (int c = 0; c < 8; ++c) v[c] = i0 + c * 64 + lane < m ? v[c] : ~0u;
         u32 bound = ~0u;
         if (list.limit == ~0ULL && m - i0 > list.want) {
             // the want-th of the words, or of the lanes' smallest words: at least want of the words do not exceed either, and
@@ -702,62 +712,78 @@ __device__ inline void choose(KeyList &list, int m, int lane, Word word, Name na
     }
 }
 
-// u of the 16 rows from row0 (the same for all lanes) on: start values, then products of S steps whose operands are
-// loaded together, TILES tiles side by side.  row0 is a row of the table; rows past its end have u = inf.
-template <int S, int TILES>
-__device__ inline void score_tiles(const Table &t, const Table &q, const Operand &first, int qrow, int r, int g, const int (&row0)[TILES],
-                                   f32x4 (&acc)[TILES])
+// u of the 16 rows from row0 (the same for all lanes) on, four tiles side by side, S steps at a time through the wave's own
+// piece of LDS.  row0 is a row of the table; rows past its end have u = inf.
+template <int S>
+struct ScoreLds {
+    u32 codes[4 * S][256];
+    u32 scales[S][4][16];
+};
+template <int S>
+__device__ inline void score_tiles(const Table &t, const Table &q, ScoreLds<S> *lds, const Operand &first, int qrow, int lane,
+                                   const int (&row0)[4], f32x4 (&acc)[4])
 {
-    const int steps = (t.nb + 3) / 4;
-    int row[TILES];
-    bool ok[TILES], odd = false;
+    const int steps = (t.nb + 3) / 4, r = lane & 15, g = lane >> 4, at_lane = mx_staged_at(r, g);
+    bool ok[4] = {true, true, true, true};
+    const bool whole = max(max(row0[0], row0[1]), max(row0[2], row0[3])) + 16 <= t.n;
+    const int last_row = g == 0 ? row0[0] : g == 1 ? row0[1] : g == 2 ? row0[2] : row0[3];
+    const uint8_t *lane_scales = t.scales + (size_t)min(last_row + r, t.n - 1) * t.sp;
+    const auto stage = [&](int s0) {
 #pragma unroll
-    for (int i = 0; i < TILES; ++i) {
-        const int left = t.n - row0[i];
-        row[i] = min(r, left - 1);
-        // (as few loads as there can be: what returns them is busy 9 cycles of 10 where many queries pick)
-        acc[i] = f32x4{__builtin_inff(), 0.0f, 0.0f, 0.0f};
-        if (left >= 16) acc[i] = *(const f32x4 *)(t.norms + row0[i] + 4 * g);
+        for (int s = 0; s < S; ++s) {
+            if (S > 1 && s0 + s >= steps) break;
+            const int block = mx_stage_block(lane, s0 + s, t.nb);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) odd |= !mx_takes_part(acc[i][c]);
-        ok[i] = true;
+            for (int i = 0; i < 4; ++i) {
+                const int row = whole ? lane >> 2 : min(lane >> 2, t.n - 1 - row0[i]);
+                mx_stage(t.codes + (size_t)row0[i] * t.nb * 16 + (u32)(__umul24(row, t.nb) + block) * 16, &lds->codes[s * 4 + i][0], 1);
+            }
+            mx_stage(lane_scales + 4 * (s0 + s), &lds->scales[s][0][0], 0);
+        }
+    };
+    stage(0);
+    float top = 0.0f;
+    if (whole) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] = *(const f32x4 *)(t.norms + row0[i] + 4 * g);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            top = __builtin_elementwise_maximum(__builtin_elementwise_maximum(top, __builtin_elementwise_maximum(acc[i][0], acc[i][1])),
+                                                __builtin_elementwise_maximum(acc[i][2], acc[i][3]));      // (a NaN stays)
     }
-    if (__any(odd)) {
+    if (!whole || __any(!mx_takes_part(top))) {
 #pragma unroll
-        for (int i = 0; i < TILES; ++i) {
+        for (int i = 0; i < 4; ++i) {
             const int left = t.n - row0[i];
             const float *norms = t.norms + row0[i];
             const auto start = [&](int c) {
                 const float norm = norms[min(4 * g + c, left - 1)];
                 return 4 * g + c < left && mx_takes_part(norm) ? norm : __builtin_inff();
             };
-            ok[i] = mx_takes_part(norms[row[i]]);
+            ok[i] = mx_takes_part(norms[min(r, left - 1)]);
             acc[i] = f32x4{start(0), start(1), start(2), start(3)};
         }
     }
     for (int s0 = 0; s0 < steps; s0 += S) {
-        Operand y[S], x[S][TILES];
+        if (s0 > 0) stage(s0);
+        Operand y[S];
+#pragma unroll
+        for (int s = 0; s < S; ++s) y[s] = S == 1 && s0 == 0 ? first : mx_query(q, qrow, 4 * (s0 + s) + g, true);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
         for (int s = 0; s < S; ++s) {
-            const int block = 4 * (s0 + s) + g;
-            y[s] = S == 1 && s0 == 0 ? first : mx_query(q, qrow, block, true);
+            if (S > 1 && s0 + s >= steps) break;
+            const int block = min(4 * (s0 + s) + g, t.nb - 1) & 3;
 #pragma unroll
-            for (int i = 0; i < TILES; ++i) {
-                const uint8_t *codes = t.codes + (size_t)row0[i] * t.nb * 16, *scales = t.scales + (size_t)row0[i] * t.sp;
-                x[s][i] = {{0, 0, 0, 0}, 0};
-                if (block < t.nb) {
-                    x[s][i].codes = *(const i32x4 *)(codes + (u32)(__umul24(row[i], t.nb) + block) * 16);
-                    x[s][i].scale = scales[(u32)(__umul24(row[i], t.sp) + block)];
-                }
+            for (int i = 0; i < 4; ++i) {
+                Operand x;
+                x.codes = *(const i32x4 *)&lds->codes[s * 4 + i][at_lane];
+                const int scale = ((const uint8_t *)&lds->scales[s][i][r])[block];
+                x.scale = ok[i] ? scale : 0;
+                acc[i] = mx_mma(x, y[s], acc[i]);
             }
         }
-#pragma unroll
-        for (int s = 0; s < S; ++s)
-#pragma unroll
-            for (int i = 0; i < TILES; ++i) {
-                if (!ok[i]) x[s][i].scale = 0;
-                acc[i] = mx_mma(x[s][i], y[s], acc[i]);
-            }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // (read before it is written again)
     }
 }
 
@@ -766,7 +792,7 @@ __device__ inline void score_tiles(const Table &t, const Table &q, const Operand
 template <int WAVES, int S>
 __global__ __launch_bounds__(64 * WAVES) void pick_kernel(Scan a, int k, long long first_self, int *ids, float *dists)
 {
-    extern __shared__ u64 lds[];
+    extern __shared__ __align__(16) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
     // sixteen neighbouring queries, whose minima lie side by side, on one chiplet (every eighth workgroup)
     const int qi = WAVES > 1 ? blockIdx.x : (blockIdx.x & ~127) + (blockIdx.x & 7) * 16 + ((blockIdx.x >> 3) & 15);
@@ -774,7 +800,8 @@ __global__ __launch_bounds__(64 * WAVES) void pick_kernel(Scan a, int k, long lo
     const int kk = k + (first_self >= 0 ? 1 : 0), group = 4 * a.tiles;
     const Table &t = a.t, &q = a.q;
     const int self = first_self >= 0 ? (int)min(first_self + a.first + qi, 0x7FFFFFFFLL) : -1;
-    u64 *mine = lds + wave * (2 * kk + kListRoom);
+    ScoreLds<S> *scores = (ScoreLds<S> *)lds + wave;
+    u64 *lists = (u64 *)((ScoreLds<S> *)lds + WAVES), *mine = lists + wave * (2 * kk + kListRoom);
     u64 *chosen = mine + kk + kListRoom;
     int *out_ids = ids + (size_t)(a.first + qi) * k;
     float *out_dists = dists + (size_t)(a.first + qi) * k;
@@ -814,7 +841,7 @@ __global__ __launch_bounds__(64 * WAVES) void pick_kernel(Scan a, int k, long lo
                 live[i] = tile0 + i < n_tiles && row0[i] < t.n;      // (the table can end inside a group)
                 row0[i] = live[i] ? row0[i] : 0;
             }
-            score_tiles<S, 4>(t, q, first, a.first + qi, r, g, row0, acc);
+            score_tiles<S>(t, q, scores, first, a.first + qi, lane, row0, acc);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float u = r == 0 ? acc[i][0] : r == 1 ? acc[i][1] : r == 2 ? acc[i][2] : acc[i][3];
@@ -824,18 +851,18 @@ __global__ __launch_bounds__(64 * WAVES) void pick_kernel(Scan a, int k, long lo
             }
             if (list.count > kListRoom - 64) list.cut(lane);
         }
-        list.cut(lane);
     }
     if (WAVES > 1) {
+        if (list.count > kk) list.cut(lane);
         __shared__ int counts[WAVES];
         if (lane == 0) counts[wave] = list.count;
         __syncthreads();
         if (wave != 0) return;
         for (int w = 1; w < WAVES; ++w) {
-            const u64 *theirs = lds + w * (2 * kk + kListRoom);
+            const u64 *theirs = lists + w * (2 * kk + kListRoom);
             const int c = counts[w];
             for (int i0 = 0; i0 < c; i0 += 64) list.push(i0 + lane < c ? theirs[i0 + lane] : 0, i0 + lane < c, lane);
-            if (list.count > kListRoom - 256 || w == WAVES - 1) list.cut(lane);
+            if (list.count > kListRoom - 256) list.cut(lane);
         }
     }
     list.sort(lane);
@@ -877,7 +904,7 @@ inline NearestShape nearest_shape(int64_t n, int64_t nq, int k)
 template <int WAVES, int S>
 int launch_pick_of(const Scan &a, int k, int64_t first_self, int32_t *ids, float *dists, hipStream_t st)
 {
-    const int kk = k + (first_self >= 0 ? 1 : 0), lds = WAVES * (2 * kk + kListRoom) * 8;
+    const int kk = k + (first_self >= 0 ? 1 : 0), lds = WAVES * ((2 * kk + kListRoom) * 8 + (int)sizeof(ScoreLds<S>));
     EF_HIP_CHECK(hipFuncSetAttribute((const void *)pick_kernel<WAVES, S>, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
     const int blocks = WAVES > 1 ? a.nq : (a.nq + 127) & ~127;
     pick_kernel<WAVES, S><<<(unsigned)blocks, 64 * WAVES, lds, st>>>(a, k, first_self, ids, dists);
@@ -894,7 +921,7 @@ int launch_pick(const Scan &a, int k, int64_t first_self, int32_t *ids, float *d
 template <int KS, int QF>
 int launch_wide(Scan a, hipStream_t st)
 {
-    const int lds = 2 * (int)sizeof(StageLds<KS>);
+    const int lds = 2 * (int)sizeof(StageLds<KS == 1 ? kStage : KS == 2 ? kStage / 2 : KS <= 4 ? kStage / 4 : kStage / 8, KS>);
     EF_HIP_CHECK(hipFuncSetAttribute((const void *)scan_wide_kernel<KS, QF>, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
     a.q_parts = (a.nq + 128 * QF - 1) / (128 * QF);
     // supers per workgroup: enough for its queries' loads to be little next to its rows', few enough to fill the CUs (two workgroups
@@ -911,7 +938,9 @@ int launch_wide(Scan a, hipStream_t st)
 template <int KS, int QF>
 int launch_narrow(const Scan &a, hipStream_t st)
 {
-    scan_narrow_kernel<KS, QF><<<dim3((unsigned)a.supers, (unsigned)((a.nq + 16 * QF - 1) / (16 * QF))), 256, 0, st>>>(a);
+    const int lds = 4 * (int)sizeof(StageLds<KS == 1 ? 16 : KS == 2 ? 8 : KS <= 4 ? 4 : 2, KS>);
+    EF_HIP_CHECK(hipFuncSetAttribute((const void *)scan_narrow_kernel<KS, QF>, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+    scan_narrow_kernel<KS, QF><<<dim3((unsigned)a.supers, (unsigned)((a.nq + 16 * QF - 1) / (16 * QF))), 256, lds, st>>>(a);
     return EFANNA_OK;
 }
 template <int KS>
@@ -1043,7 +1072,7 @@ extern "C" int efanna_mx_nearest(const uint8_t *codes, const uint8_t *scales, co
             if (rc != EFANNA_OK) return rc;
             EF_HIP_CHECK(hipGetLastError());
         }
-        const int rc = a.t.nb <= 4 ? launch_pick<1>(a, k, first_self, ids, dists, st) : launch_pick<4>(a, k, first_self, ids, dists, st);
+        const int rc = a.t.nb <= 4 ? launch_pick<1>(a, k, first_self, ids, dists, st) : launch_pick<2>(a, k, first_self, ids, dists, st);
         if (rc != EFANNA_OK) return rc;
         EF_HIP_CHECK(hipGetLastError());
     }
