@@ -145,41 +145,309 @@ __device__ inline f32x4 mx_mma(const Operand &a, const Operand &b, f32x4 c)
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a8, b8, c, kFp4, kFp4, 0, a.scale, 0, b.scale);
 }
 
+typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((address_space(1))) const void global_void;
+
+// Rows pass through LDS by loads that write there directly.  An operand (16 rows, a step's 4 blocks) is 1 KiB; lane l of
+// its load brings a 16-byte block of row l / 4, so that four lanes share 64 consecutive bytes of memory (with the lanes in the
+// order the matrix instruction wants them the loads return a quarter as fast).  The blocks of row r lie in the order
+// b ^ (r / 2) % 4, so that blocks b of eight neighbouring rows, which are read together, are in different banks.
+__device__ inline int mx_stage_block(int lane, int step, int nb) { return min(4 * step + ((lane & 3) ^ ((lane >> 3) & 3)), nb - 1); }
+__device__ inline int mx_staged_at(int r, int g) { return (r * 4 + (g ^ ((r >> 1) & 3))) * 4; }      // word within the operand
+__device__ inline void mx_stage(const void *from, void *to, int lane_bytes_16)
+{
+    if (lane_bytes_16) __builtin_amdgcn_global_load_lds((global_void *)from, (lds_void *)to, 16, 0, 0);
+    else __builtin_amdgcn_global_load_lds((global_void *)from, (lds_void *)to, 4, 0, 0);
+}
+
 // ---- product ---------------------------------------------------------------------------------------------
 // out[i][j] = a_i . b_j.  The rows of b are the instruction's rows and those of a its columns, so that a lane
-// ends up with four consecutive values of an output row.  A wave: 64 rows of a by 64 of b.
+// ends up with four consecutive values of an output row.
 template <class T>
-__global__ __launch_bounds__(256) void product_kernel(Table a, Table b, T *out, long long ldo)
+__device__ inline void store_four(T *o, f32x4 x, int left)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
-    const int j0 = (blockIdx.x * 2 + (wave & 1)) * 64, i0 = (blockIdx.y * 2 + (wave >> 1)) * 64;
-    if (i0 >= a.n || j0 >= b.n) return;
-    f32x4 acc[4][4] = {};
-    for (int s = 0; s < (a.nb + 3) / 4; ++s) {
-        Operand oa[4], ob[4];
+    if (left >= 4) {
+        typedef T Unaligned __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+        *(Unaligned *)o = Unaligned{from_float<T>(x[0]), from_float<T>(x[1]), from_float<T>(x[2]), from_float<T>(x[3])};
+    } else
 #pragma unroll
-        for (int f = 0; f < 4; ++f) {
-            oa[f] = mx_load(a, min(i0 + 16 * f + r, a.n - 1), 4 * s + g);
-            ob[f] = mx_load(b, min(j0 + 16 * f + r, b.n - 1), 4 * s + g);
+        for (int c = 0; c < 4; ++c)
+            if (c < left) o[c] = from_float<T>(x[c]);
+}
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+template <int N> __device__ inline void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+
+// WA x WB waves share a tile of a's rows by b's rows, FA x FB instructions of 32 x 32 x 64 each.  A stage is a step of
+// 128 coordinates of both; while one is computed the next two are on their way into LDS.
+constexpr int kBuffers = 3;
+template <int FA, int FB, int WA, int WB>
+struct Tiling {
+    static constexpr int waves = WA * WB, side_a = 32 * FA * WA, side_b = 32 * FB * WB;
+    static constexpr int ops_a = side_a / 16, ops_b = side_b / 16;              // pieces of 16 rows
+    static constexpr int each = (ops_a + ops_b) / waves;                        // pieces that a wave loads
+    static constexpr int words = (side_a + side_b) / 64, each_words = (words + waves - 1) / waves;
+    static_assert((ops_a + ops_b) % waves == 0, "every wave loads as much");
+    struct Lds {
+        u32 codes[ops_a + ops_b][256];      // a's pieces, then b's
+        u32 scales[side_a + side_b];        // a word per row
+    };
+    static constexpr int out_pitch = 32 * FB + 8;       // values of a row of the piece that a wave turns round at the end
+};
+
+template <class T, int FA, int FB, int WA, int WB>
+__global__ __launch_bounds__(64 * WA * WB, FA * FB > 8 ? 1 : 2) void product_tile_kernel(Table a, Table b, T *out, long long ldo, int tiles_a,
+                                                                                          int tiles_b)
+{
+    typedef Tiling<FA, FB, WA, WB> Tile;
+    typedef typename Tile::Lds Lds;
+    extern __shared__ __align__(16) char lds_raw[];
+    Lds *stage = (Lds *)lds_raw;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 31, half = lane >> 5;
+    // A chiplet (every eighth workgroup) gets a connected piece of the tiles, walked in strips of eight rows of tiles: what runs
+    // there together shares rows of a and of b in its L2.
+    int ta, tb;
+    {
+        const int all = tiles_a * tiles_b, each = all / 8, more = all % 8, xcd = blockIdx.x & 7;
+        const int at = xcd * each + min(xcd, more) + (blockIdx.x >> 3);
+        const int strip = at / (8 * tiles_b), high = min(8, tiles_a - strip * 8), in = at - strip * 8 * tiles_b;
+        ta = strip * 8 + in % high;
+        tb = in / high;
+    }
+    const int i0 = ta * Tile::side_a, j0 = tb * Tile::side_b;
+    const int rows_a = a.n - i0, rows_b = b.n - j0, steps = (a.nb + 3) / 4;
+    const uint8_t *codes_a = a.codes + (size_t)i0 * a.nb * 16, *codes_b = b.codes + (size_t)j0 * b.nb * 16;
+    const uint8_t *scales_a = a.scales + (size_t)i0 * a.sp, *scales_b = b.scales + (size_t)j0 * b.sp;
+    u32 at_codes[Tile::each], at_scales[Tile::each_words];
+#pragma unroll
+    for (int i = 0; i < Tile::each; ++i) {
+        const int op = wave * Tile::each + i, row = (lane >> 2) + 16 * (op < Tile::ops_a ? op : op - Tile::ops_a);
+        at_codes[i] = (u32)min(row, (op < Tile::ops_a ? rows_a : rows_b) - 1) * a.nb * 16;
+    }
+#pragma unroll
+    for (int i = 0; i < Tile::each_words; ++i) {
+        const int row = (wave * Tile::each_words + i) * 64 + lane;
+        at_scales[i] = (u32)(row < Tile::side_a ? min(row, rows_a - 1) : min(row - Tile::side_a, rows_b - 1)) * a.sp;
+    }
+    const auto load = [&](int step) {
+        Lds *to = stage + step % kBuffers;
+        const u32 block = mx_stage_block(lane, step, a.nb) * 16;
+#pragma unroll
+        for (int i = 0; i < Tile::each; ++i) {
+            const int op = wave * Tile::each + i;
+            mx_stage((op < Tile::ops_a ? codes_a : codes_b) + at_codes[i] + block, &to->codes[op][0], 1);
         }
 #pragma unroll
-        for (int y = 0; y < 4; ++y)
-#pragma unroll
-            for (int x = 0; x < 4; ++x) acc[y][x] = mx_mma(ob[x], oa[y], acc[y][x]);
-    }
-#pragma unroll
-    for (int y = 0; y < 4; ++y) {
-        const int i = i0 + 16 * y + r;
-        if (i >= a.n) continue;
-        T *o = out + (size_t)i * ldo;
-#pragma unroll
-        for (int x = 0; x < 4; ++x)
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const int j = j0 + 16 * x + 4 * g + c;
-                if (j < b.n) o[j] = from_float<T>(acc[y][x][c]);
+        for (int i = 0; i < Tile::each_words; ++i) {
+            const int op = wave * Tile::each_words + i;
+            if (Tile::words % Tile::waves == 0 || op < Tile::words)
+                mx_stage((op * 64 < Tile::side_a ? scales_a : scales_b) + at_scales[i] + 4 * step, &to->scales[op * 64], 0);
+        }
+    };
+    constexpr int kLoads = Tile::each + Tile::words / Tile::waves;      // per stage and wave, at least
+    f32x16 acc[FA][FB] = {};
+    const int wa = wave % WA * 32 * FA, wb = wave / WA * 32 * FB;
+    load(0);
+    if (steps > 1) load(1);
+    for (int step = 0; step < steps; ++step) {
+        // this stage has arrived (what is still out belongs to the next), and what was read of the one before it is in registers
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (step + 1 < steps) wait_loads<kLoads>();
+        else wait_loads<0>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (step + 2 < steps) load(step + 2);
+        Lds *now = stage + step % kBuffers;
+        if (step + 1 == steps && (a.nb & 3)) {
+            // blocks past the last one: nothing in a, and no scale of either
+            const int have = a.nb & 3;
+            for (int i = tid; i < Tile::side_a * (4 - have); i += 64 * Tile::waves) {
+                const int row = i / (4 - have), block = have + i % (4 - have);
+                *(i32x4 *)&now->codes[row >> 4][mx_staged_at(row & 15, block)] = i32x4{0, 0, 0, 0};
             }
+            for (int i = tid; i < Tile::side_a + Tile::side_b; i += 64 * Tile::waves) now->scales[i] &= (1u << (8 * have)) - 1;
+            __syncthreads();
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            Operand oa[FA], ob[FB];
+            const int block = 2 * h + half;
+#pragma unroll
+            for (int f = 0; f < FA; ++f) {
+                const int row = wa + 32 * f + r;
+                oa[f].codes = *(const i32x4 *)&now->codes[row >> 4][mx_staged_at(r & 15, block)];
+                oa[f].scale = ((const uint8_t *)&now->scales[row])[block];
+            }
+#pragma unroll
+            for (int f = 0; f < FB; ++f) {
+                const int row = Tile::side_a + wb + 32 * f + r;
+                ob[f].codes = *(const i32x4 *)&now->codes[row >> 4][mx_staged_at(r & 15, block)];
+                ob[f].scale = ((const uint8_t *)&now->scales[row])[block];
+            }
+#pragma unroll
+            for (int y = 0; y < FA; ++y)
+#pragma unroll
+                for (int x = 0; x < FB; ++x) {
+                    const i32x8 a8 = {ob[x].codes.x, ob[x].codes.y, ob[x].codes.z, ob[x].codes.w, 0, 0, 0, 0};
+                    const i32x8 b8 = {oa[y].codes.x, oa[y].codes.y, oa[y].codes.z, oa[y].codes.w, 0, 0, 0, 0};
+                    acc[y][x] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a8, b8, acc[y][x], kFp4, kFp4, 0, ob[x].scale, 0, oa[y].scale);
+                }
+        }
     }
+    // Out through LDS, 32 rows of a wave's piece at a time, so that stores are whole rows of it.  (Straight from the registers
+    // a store instruction is 64 pieces of 8 or 16 bytes: 65 536 x 4096 of 16 bits took 1.9 ms.)
+    __syncthreads();
+    constexpr int kAcross = 32 * FB, kPitch = Tile::out_pitch, kPer = 16 / sizeof(T), kLanes = kAcross / kPer;      // lanes per row
+    T *turn = (T *)lds_raw + wave * 32 * kPitch;
+    typedef T Out __attribute__((ext_vector_type(kPer), aligned(sizeof(T))));
+    typedef T Turn __attribute__((ext_vector_type(4), aligned(8)));
+#pragma unroll
+    for (int y = 0; y < FA; ++y) {
+#pragma unroll
+        for (int x = 0; x < FB; ++x)
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                *(Turn *)&turn[r * kPitch + 32 * x + 8 * c + 4 * half] =
+                    Turn{from_float<T>(acc[y][x][4 * c]), from_float<T>(acc[y][x][4 * c + 1]), from_float<T>(acc[y][x][4 * c + 2]),
+                         from_float<T>(acc[y][x][4 * c + 3])};
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
+        const int j = lane % kLanes * kPer, left = rows_b - wb - j;
+#pragma unroll
+        for (int i = lane / kLanes; i < 32; i += 64 / kLanes) {
+            const int row = wa + 32 * y + i;
+            if (row >= rows_a) continue;
+            T *o = out + (size_t)(i0 + row) * ldo + j0 + wb + j;
+            const T *from = &turn[i * kPitch + j];
+            if (left >= kPer) *(Out *)o = *(const Out *)from;
+            else
+                for (int c = 0; c < left; ++c) o[c] = from[c];
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// Few rows of a (16 * M at most): bound by reading b once.  A wave takes 64 rows of b and its share of the steps, S of them in
+// flight; the WAVES waves of a workgroup take the same rows, and their sums meet in LDS, in the waves' order.
+template <int S>
+struct FewLds {
+    u32 codes[4 * S][256];
+    u32 scales[S][4][16];
+};
+template <class T, int M, int S, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void product_few_kernel(Table a, Table b, T *out, long long ldo)
+{
+    extern __shared__ __align__(16) char lds_raw[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
+    FewLds<S> *lds = (FewLds<S> *)lds_raw + wave;
+    const int j0 = blockIdx.x * 64, left = b.n - j0, at_lane = mx_staged_at(r, g);
+    const int steps = (a.nb + 3) / 4, s_lo = steps * wave / WAVES, s_hi = steps * (wave + 1) / WAVES;
+    const uint8_t *from_codes = b.codes + (size_t)j0 * b.nb * 16, *lane_scales = b.scales + (size_t)(j0 + min(lane, left - 1)) * b.sp;
+    u32 at_codes[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) at_codes[i] = (u32)min(16 * i + (lane >> 2), left - 1) * b.nb * 16;
+    f32x4 acc[M][4] = {};
+    for (int s0 = s_lo; s0 < s_hi; s0 += S) {
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            if (S > 1 && s0 + s >= s_hi) break;
+            const u32 block = mx_stage_block(lane, s0 + s, b.nb) * 16;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mx_stage(from_codes + at_codes[i] + block, &lds->codes[s * 4 + i][0], 1);
+            mx_stage(lane_scales + 4 * (s0 + s), &lds->scales[s][0][0], 0);
+        }
+        Operand y[S][M];
+#pragma unroll
+        for (int s = 0; s < S; ++s)
+#pragma unroll
+            for (int f = 0; f < M; ++f) y[s][f] = mx_load(a, min(16 * f + r, a.n - 1), 4 * (s0 + s) + g);
+        wait_loads<0>();
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            if (S > 1 && s0 + s >= s_hi) break;
+            // (missing blocks: zeros of a meet the row's last block)
+            const int block = min(4 * (s0 + s) + g, b.nb - 1) & 3;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                Operand x;
+                x.codes = *(const i32x4 *)&lds->codes[s * 4 + i][at_lane];
+                const int scale = ((const uint8_t *)&lds->scales[s][i][r])[block];
+                x.scale = 4 * (s0 + s) + g < b.nb ? scale : 0;
+#pragma unroll
+                for (int f = 0; f < M; ++f) acc[f][i] = mx_mma(x, y[s][f], acc[f][i]);
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // (read before it is written again)
+    }
+    if (WAVES > 1) {
+        f32x4 *share = (f32x4 *)lds_raw;          // [wave - 1][M * 4][lane]
+        __syncthreads();
+        if (wave > 0)
+#pragma unroll
+            for (int f = 0; f < M; ++f)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) share[((wave - 1) * M * 4 + f * 4 + i) * 64 + lane] = acc[f][i];
+        __syncthreads();
+        if (wave > 0) return;
+        for (int w = 0; w < WAVES - 1; ++w)
+#pragma unroll
+            for (int f = 0; f < M; ++f)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const f32x4 other = share[(w * M * 4 + f * 4 + i) * 64 + lane];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) acc[f][i][c] += other[c];
+                }
+    }
+#pragma unroll
+    for (int f = 0; f < M; ++f) {
+        const int i = 16 * f + r;
+        if (i >= a.n) continue;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int j = 16 * t + 4 * g;
+            if (j < left) store_four(out + (size_t)i * ldo + j0 + j, acc[f][t], left - j);
+        }
+    }
+}
+
+template <class T, int FA, int FB, int WA, int WB>
+int launch_tiles(const Table &a, const Table &b, T *out, int64_t ldo, hipStream_t st)
+{
+    typedef Tiling<FA, FB, WA, WB> Tile;
+    const int stages = kBuffers * (int)sizeof(typename Tile::Lds), turn = Tile::waves * 32 * Tile::out_pitch * (int)sizeof(T);
+    const int lds = stages > turn ? stages : turn;
+    EF_HIP_CHECK(hipFuncSetAttribute((const void *)product_tile_kernel<T, FA, FB, WA, WB>, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+    const int64_t ta = (a.n + Tile::side_a - 1) / Tile::side_a, tb = (b.n + Tile::side_b - 1) / Tile::side_b;
+    if (ta * tb > 2147483647LL) return EFANNA_EUNSUPPORTED;
+    product_tile_kernel<T, FA, FB, WA, WB><<<(unsigned)(ta * tb), 64 * Tile::waves, lds, st>>>(a, b, out, ldo, (int)ta, (int)tb);
+    return EFANNA_OK;
+}
+template <class T, int M, int S, int WAVES>
+int launch_few(const Table &a, const Table &b, T *out, int64_t ldo, hipStream_t st)
+{
+    const int stage = WAVES * (int)sizeof(FewLds<S>), join = (WAVES - 1) * M * 4 * 64 * 16, lds = stage > join ? stage : join;
+    EF_HIP_CHECK(hipFuncSetAttribute((const void *)product_few_kernel<T, M, S, WAVES>, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+    product_few_kernel<T, M, S, WAVES><<<(unsigned)((b.n + 63) / 64), 64 * WAVES, lds, st>>>(a, b, out, ldo);
+    return EFANNA_OK;
+}
+template <class T, int M>
+int launch_few_of(const Table &a, const Table &b, T *out, int64_t ldo, hipStream_t st)
+{
+    const int steps = (a.nb + 3) / 4;
+    if (steps == 1) return launch_few<T, M, 1, 1>(a, b, out, ldo, st);
+    if (steps < 8) return launch_few<T, M, 2, 1>(a, b, out, ldo, st);
+    return launch_few<T, M, 2, 4>(a, b, out, ldo, st);
+}
+template <class T>
+int launch_product(const Table &a, const Table &b, T *out, int64_t ldo, hipStream_t st)
+{
+    if (a.n <= 16) return launch_few_of<T, 1>(a, b, out, ldo, st);
+    if (a.n <= 32) return launch_few_of<T, 2>(a, b, out, ldo, st);
+    // the larger tile reads half as much from LDS and L2 per operation; the smaller one where there is less than one of those per CU
+    const int64_t large = (int64_t)((a.n + 255) / 256) * ((b.n + 255) / 256);
+    return large >= 200 ? launch_tiles<T, 4, 2, 2, 4>(a, b, out, ldo, st) : launch_tiles<T, 2, 2, 2, 2>(a, b, out, ldo, st);
 }
 
 // ---- nearest rows ----------------------------------------------------------------------------------------
@@ -196,9 +464,6 @@ __global__ __launch_bounds__(256) void product_kernel(Table a, Table b, T *out, 
 // Four groups are passed over together ("block"): tile t of `tiles` holds as instruction row r the block's row
 // (r / 4) * 4 tiles + 4 t + r % 4, so that the four values of a lane belong to one group in every tile and its
 // running minimum needs no other lane.  A group is 4 tiles rows, a super four blocks.
-typedef __attribute__((address_space(3))) void lds_void;
-typedef __attribute__((address_space(1))) const void global_void;
-
 constexpr float kNormLimit = 8.507059173023462e37f;      // 2^126
 __device__ inline bool mx_takes_part(float norm) { return norm < kNormLimit; }
 __device__ inline float mx_min(float a, float b) { return __builtin_elementwise_minimum(a, b); }
@@ -340,18 +605,6 @@ struct Queries {
     }
 };
 
-
-// Rows pass through LDS by loads that write there directly.  An operand (16 rows, a step's 4 blocks) is 1 KiB; lane l of
-// its load brings a 16-byte block of row l / 4, so that four lanes share 64 consecutive bytes of memory (with the lanes in the
-// order the matrix instruction wants them the loads return a quarter as fast).  The blocks of row r lie in the order
-// b ^ (r / 4), so that the 16 rows' blocks b, which are read together, are in different banks.
-__device__ inline int mx_stage_block(int lane, int step, int nb) { return min(4 * step + ((lane & 3) ^ (lane >> 4)), nb - 1); }
-__device__ inline int mx_staged_at(int r, int g) { return (r * 4 + (g ^ (r >> 2))) * 4; }      // word within the operand
-__device__ inline void mx_stage(const void *from, void *to, int lane_bytes_16)
-{
-    if (lane_bytes_16) __builtin_amdgcn_global_load_lds((global_void *)from, (lds_void *)to, 16, 0, 0);
-    else __builtin_amdgcn_global_load_lds((global_void *)from, (lds_void *)to, 4, 0, 0);
-}
 
 template <int TILES, int KS>
 struct StageLds {
@@ -1034,9 +1287,9 @@ extern "C" int efanna_mx_product(const uint8_t *a_codes, const uint8_t *a_scales
     hipStream_t st = (hipStream_t)stream;
     const int nb = mx_blocks(d), sp = mx_scale_pitch(d);
     const Table a = {a_codes, a_scales, nullptr, (int)m, nb, sp}, b = {b_codes, b_scales, nullptr, (int)n, nb, sp};
-    const dim3 grid((unsigned)((n + 127) / 128), (unsigned)((m + 127) / 128));
-    if (grid.y > 65535) return EFANNA_EUNSUPPORTED;
-    EF_MX_DTYPE(dtype, T, (product_kernel<T><<<grid, 256, 0, st>>>(a, b, (T *)out, ldo)));
+    int rc = EFANNA_OK;
+    EF_MX_DTYPE(dtype, T, rc = launch_product<T>(a, b, (T *)out, ldo, st));
+    if (rc != EFANNA_OK) return rc;
     EF_HIP_CHECK(hipGetLastError());
     return EFANNA_OK;
 }
