@@ -178,31 +178,29 @@ __device__ inline void store_four(T *o, f32x4 x, int left)
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 template <int N> __device__ inline void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
-// WA x WB waves share a tile of a's rows by b's rows, FA x FB instructions of 32 x 32 x 64 each.  A stage is a step of
-// 128 coordinates of both; while one is computed the next two are on their way into LDS.
-constexpr int kBuffers = 3;
+// WA x WB waves share a tile of a's rows by b's rows, FA x FB instructions of 32 x 32 x 64 each.  A stage is 256
+// coordinates of both, whole lines of 128 bytes (half lines cost the loads as much each); while one is computed the next is on
+// its way into LDS.  A load brings 8 rows; the blocks of row r lie in the order b ^ r % 8, so that blocks b of eight rows, which
+// are read together, are in different banks.
 template <int FA, int FB, int WA, int WB>
 struct Tiling {
-    static constexpr int waves = WA * WB, side_a = 32 * FA * WA, side_b = 32 * FB * WB;
-    static constexpr int ops_a = side_a / 16, ops_b = side_b / 16;              // pieces of 16 rows
-    static constexpr int each = (ops_a + ops_b) / waves;                        // pieces that a wave loads
-    static constexpr int words = (side_a + side_b) / 64, each_words = (words + waves - 1) / waves;
-    static_assert((ops_a + ops_b) % waves == 0, "every wave loads as much");
+    static constexpr int waves = WA * WB, side_a = 32 * FA * WA, side_b = 32 * FB * WB, sides = side_a + side_b;
+    static constexpr int each = sides / 8 / waves, each_words = sides / 32 / waves;      // loads of a wave: codes, scales
+    static_assert(sides % (64 * waves) == 0, "every wave loads as much");
     struct Lds {
-        u32 codes[ops_a + ops_b][256];      // a's pieces, then b's
-        u32 scales[side_a + side_b];        // a word per row
+        u32 codes[sides / 8][256];      // a's rows, then b's
+        u32 scales[2][sides];           // of blocks 0..3 and 4..7
     };
     static constexpr int out_pitch = 32 * FB + 8;       // values of a row of the piece that a wave turns round at the end
 };
 
 template <class T, int FA, int FB, int WA, int WB>
-__global__ __launch_bounds__(64 * WA * WB, FA * FB > 8 ? 1 : 2) void product_tile_kernel(Table a, Table b, T *out, long long ldo, int tiles_a,
-                                                                                          int tiles_b)
+__global__ __launch_bounds__(64 * WA * WB, 2) void product_tile_kernel(Table a, Table b, T *out, long long ldo, int tiles_a, int tiles_b)
 {
     typedef Tiling<FA, FB, WA, WB> Tile;
     typedef typename Tile::Lds Lds;
     extern __shared__ __align__(16) char lds_raw[];
-    Lds *stage = (Lds *)lds_raw;
+    Lds *stages = (Lds *)lds_raw;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 31, half = lane >> 5;
     // A chiplet (every eighth workgroup) gets a connected piece of the tiles, walked in strips of eight rows of tiles: what runs
     // there together shares rows of a and of b in its L2.
@@ -215,83 +213,103 @@ __global__ __launch_bounds__(64 * WA * WB, FA * FB > 8 ? 1 : 2) void product_til
         tb = in / high;
     }
     const int i0 = ta * Tile::side_a, j0 = tb * Tile::side_b;
-    const int rows_a = a.n - i0, rows_b = b.n - j0, steps = (a.nb + 3) / 4;
+    const int rows_a = a.n - i0, rows_b = b.n - j0, n_stages = (a.nb + 7) / 8;
     const uint8_t *codes_a = a.codes + (size_t)i0 * a.nb * 16, *codes_b = b.codes + (size_t)j0 * b.nb * 16;
     const uint8_t *scales_a = a.scales + (size_t)i0 * a.sp, *scales_b = b.scales + (size_t)j0 * b.sp;
     u32 at_codes[Tile::each], at_scales[Tile::each_words];
 #pragma unroll
     for (int i = 0; i < Tile::each; ++i) {
-        const int op = wave * Tile::each + i, row = (lane >> 2) + 16 * (op < Tile::ops_a ? op : op - Tile::ops_a);
-        at_codes[i] = (u32)min(row, (op < Tile::ops_a ? rows_a : rows_b) - 1) * a.nb * 16;
+        const int row = (wave * Tile::each + i) * 8 + (lane >> 3);
+        at_codes[i] = (u32)(row < Tile::side_a ? min(row, rows_a - 1) : min(row - Tile::side_a, rows_b - 1)) * a.nb * 16;
     }
 #pragma unroll
     for (int i = 0; i < Tile::each_words; ++i) {
-        const int row = (wave * Tile::each_words + i) * 64 + lane;
+        const int row = (wave * Tile::each_words + i) * 64 % Tile::sides + lane;
         at_scales[i] = (u32)(row < Tile::side_a ? min(row, rows_a - 1) : min(row - Tile::side_a, rows_b - 1)) * a.sp;
     }
-    const auto load = [&](int step) {
-        Lds *to = stage + step % kBuffers;
-        const u32 block = mx_stage_block(lane, step, a.nb) * 16;
+    const auto load = [&](int stage) {
+        Lds *to = stages + (stage & 1);
+        const u32 block = min(8 * stage + ((lane & 7) ^ (lane >> 3)), a.nb - 1) * 16;
 #pragma unroll
         for (int i = 0; i < Tile::each; ++i) {
             const int op = wave * Tile::each + i;
-            mx_stage((op < Tile::ops_a ? codes_a : codes_b) + at_codes[i] + block, &to->codes[op][0], 1);
+            mx_stage((op * 8 < Tile::side_a ? codes_a : codes_b) + at_codes[i] + block, &to->codes[op][0], 1);
         }
 #pragma unroll
         for (int i = 0; i < Tile::each_words; ++i) {
-            const int op = wave * Tile::each_words + i;
-            if (Tile::words % Tile::waves == 0 || op < Tile::words)
-                mx_stage((op * 64 < Tile::side_a ? scales_a : scales_b) + at_scales[i] + 4 * step, &to->scales[op * 64], 0);
+            const int op = wave * Tile::each_words + i, row = op * 64 % Tile::sides, word = op * 64 / Tile::sides;
+            mx_stage((row < Tile::side_a ? scales_a : scales_b) + at_scales[i] + min(8 * stage + 4 * word, a.sp - 4), &to->scales[word][row], 0);
         }
     };
-    constexpr int kLoads = Tile::each + Tile::words / Tile::waves;      // per stage and wave, at least
     f32x16 acc[FA][FB] = {};
     const int wa = wave % WA * 32 * FA, wb = wave / WA * 32 * FB;
-    load(0);
-    if (steps > 1) load(1);
-    for (int step = 0; step < steps; ++step) {
-        // this stage has arrived (what is still out belongs to the next), and what was read of the one before it is in registers
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (step + 1 < steps) wait_loads<kLoads>();
-        else wait_loads<0>();
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        if (step + 2 < steps) load(step + 2);
-        Lds *now = stage + step % kBuffers;
-        if (step + 1 == steps && (a.nb & 3)) {
-            // blocks past the last one: nothing in a, and no scale of either
-            const int have = a.nb & 3;
-            for (int i = tid; i < Tile::side_a * (4 - have); i += 64 * Tile::waves) {
-                const int row = i / (4 - have), block = have + i % (4 - have);
-                *(i32x4 *)&now->codes[row >> 4][mx_staged_at(row & 15, block)] = i32x4{0, 0, 0, 0};
-            }
-            for (int i = tid; i < Tile::side_a + Tile::side_b; i += 64 * Tile::waves) now->scales[i] &= (1u << (8 * have)) - 1;
-            __syncthreads();
+    // where the lane's block of the first 64 coordinates is in a stage (block b ^ r % 8 of row r; 64 coordinates on: the
+    // offset ^ 32), and its scale; 32 rows further down 4096 and 128 bytes on
+    const int code_a = (wa + r) * 128 + (half ^ (r & 7)) * 16, code_b = (Tile::side_a + wb + r) * 128 + (half ^ (r & 7)) * 16;
+    const int scale_a = (wa + r) * 4 + half, scale_b = (Tile::side_a + wb + r) * 4 + half;
+    // 64 coordinates at a time; the next operands are read while the matrix unit works on these
+    Operand oa[2][FA], ob[2][FB];
+    const auto read = [&](const Lds *now, int h, int to) {
+        const char *ca = (const char *)now->codes + (code_a ^ (32 * h)), *cb = (const char *)now->codes + (code_b ^ (32 * h));
+        const char *sa = (const char *)now->scales[h >> 1] + scale_a + 2 * (h & 1), *sb = (const char *)now->scales[h >> 1] + scale_b + 2 * (h & 1);
+#pragma unroll
+        for (int f = 0; f < FA; ++f) {
+            oa[to][f].codes = *(const i32x4 *)(ca + 32 * 128 * f);
+            oa[to][f].scale = *(const uint8_t *)(sa + 32 * 4 * f);
         }
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            Operand oa[FA], ob[FB];
-            const int block = 2 * h + half;
+        for (int f = 0; f < FB; ++f) {
+            ob[to][f].codes = *(const i32x4 *)(cb + 32 * 128 * f);
+            ob[to][f].scale = *(const uint8_t *)(sb + 32 * 4 * f);
+        }
+    };
+    const auto multiply = [&](int from) {
 #pragma unroll
-            for (int f = 0; f < FA; ++f) {
-                const int row = wa + 32 * f + r;
-                oa[f].codes = *(const i32x4 *)&now->codes[row >> 4][mx_staged_at(r & 15, block)];
-                oa[f].scale = ((const uint8_t *)&now->scales[row])[block];
+        for (int y = 0; y < FA; ++y)
+#pragma unroll
+            for (int x = 0; x < FB; ++x) {
+                const Operand &p = ob[from][x], &q = oa[from][y];
+                const i32x8 p8 = {p.codes.x, p.codes.y, p.codes.z, p.codes.w, 0, 0, 0, 0};
+                const i32x8 q8 = {q.codes.x, q.codes.y, q.codes.z, q.codes.w, 0, 0, 0, 0};
+                acc[y][x] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(p8, q8, acc[y][x], kFp4, kFp4, 0, p.scale, 0, q.scale);
             }
+    };
+    // a stage has arrived, and what was read of the one before it is in registers
+    const auto arrived = [&]() {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    load(0);
+    int stage = 0;
+    for (; 8 * stage + 8 <= a.nb; ++stage) {
+        arrived();
+        if (stage + 1 < n_stages) load(stage + 1);
+        const Lds *now = stages + (stage & 1);
+        read(now, 0, 0);
 #pragma unroll
-            for (int f = 0; f < FB; ++f) {
-                const int row = Tile::side_a + wb + 32 * f + r;
-                ob[f].codes = *(const i32x4 *)&now->codes[row >> 4][mx_staged_at(r & 15, block)];
-                ob[f].scale = ((const uint8_t *)&now->scales[row])[block];
+        for (int h = 0; h < 4; ++h) {
+            if (h < 3) read(now, h + 1, (h + 1) & 1);
+            multiply(h & 1);
+            __builtin_amdgcn_sched_barrier(0);        // (reads further ahead do not fit the registers)
+        }
+    }
+    if (stage < n_stages) {
+        arrived();
+        Lds *now = stages + (stage & 1);
+        const int have = a.nb - 8 * stage;
+        if (have & 1) {
+            // the second half of the last instruction: nothing in a, and no scale of either
+            for (int row = tid; row < Tile::sides; row += 64 * Tile::waves) {
+                if (row < Tile::side_a) *(i32x4 *)&now->codes[row >> 3][((row & 7) * 8 + (have ^ (row & 7))) * 4] = i32x4{0, 0, 0, 0};
+                ((uint8_t *)&now->scales[have >> 2][row])[have & 3] = 0;
             }
-#pragma unroll
-            for (int y = 0; y < FA; ++y)
-#pragma unroll
-                for (int x = 0; x < FB; ++x) {
-                    const i32x8 a8 = {ob[x].codes.x, ob[x].codes.y, ob[x].codes.z, ob[x].codes.w, 0, 0, 0, 0};
-                    const i32x8 b8 = {oa[y].codes.x, oa[y].codes.y, oa[y].codes.z, oa[y].codes.w, 0, 0, 0, 0};
-                    acc[y][x] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a8, b8, acc[y][x], kFp4, kFp4, 0, ob[x].scale, 0, oa[y].scale);
-                }
+            __syncthreads();
+        }
+#pragma unroll 1
+        for (int h = 0; 2 * h < have; ++h) {
+            read(now, h, 0);
+            multiply(0);
         }
     }
     // Out through LDS, 32 rows of a wave's piece at a time, so that stores are whole rows of it.  (Straight from the registers
@@ -416,7 +434,7 @@ template <class T, int FA, int FB, int WA, int WB>
 int launch_tiles(const Table &a, const Table &b, T *out, int64_t ldo, hipStream_t st)
 {
     typedef Tiling<FA, FB, WA, WB> Tile;
-    const int stages = kBuffers * (int)sizeof(typename Tile::Lds), turn = Tile::waves * 32 * Tile::out_pitch * (int)sizeof(T);
+    const int stages = 2 * (int)sizeof(typename Tile::Lds), turn = Tile::waves * 32 * Tile::out_pitch * (int)sizeof(T);
     const int lds = stages > turn ? stages : turn;
     EF_HIP_CHECK(hipFuncSetAttribute((const void *)product_tile_kernel<T, FA, FB, WA, WB>, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
     const int64_t ta = (a.n + Tile::side_a - 1) / Tile::side_a, tb = (b.n + Tile::side_b - 1) / Tile::side_b;
