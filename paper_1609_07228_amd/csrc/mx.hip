@@ -179,28 +179,30 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 template <int N> __device__ inline void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
 // WA x WB waves share a tile of a's rows by b's rows, FA x FB instructions of 32 x 32 x 64 each.  A stage is 256
-// coordinates of both, whole lines of 128 bytes (half lines cost the loads as much each); while one is computed the next is on
-// its way into LDS.  A load brings 8 rows; the blocks of row r lie in the order b ^ r % 8, so that blocks b of eight rows, which
-// are read together, are in different banks.
+// coordinates of both, whole lines of 128 bytes (half lines cost the loads as much each), and the scales of 512 coordinates
+// with every other one; while one is computed the next is on its way into LDS.  A load of codes brings 8 rows; the blocks of row
+// r lie in the order b ^ r % 8, so that blocks b of eight rows, which are read together, are in different banks.
+// A wave reads (FA + FB) KiB from LDS for FA * FB instructions of 32 cycles; with four waves of 4 x 4 LDS is busy for 0.6 of
+// them, with eight of 4 x 2 for 0.9.
 template <int FA, int FB, int WA, int WB>
 struct Tiling {
     static constexpr int waves = WA * WB, side_a = 32 * FA * WA, side_b = 32 * FB * WB, sides = side_a + side_b;
-    static constexpr int each = sides / 8 / waves, each_words = sides / 32 / waves;      // loads of a wave: codes, scales
-    static_assert(sides % (64 * waves) == 0, "every wave loads as much");
+    static constexpr int each = sides / 8 / waves, each_scales = sides / 16 / waves;      // loads of a wave
+    static_assert(sides % (16 * waves) == 0, "every wave loads as much");
     struct Lds {
-        u32 codes[sides / 8][256];      // a's rows, then b's
-        u32 scales[2][sides];           // of blocks 0..3 and 4..7
+        u32 codes[2][sides / 8][256];       // a's rows, then b's
+        u32 scales[2][sides][4];
     };
     static constexpr int out_pitch = 32 * FB + 8;       // values of a row of the piece that a wave turns round at the end
 };
 
 template <class T, int FA, int FB, int WA, int WB>
-__global__ __launch_bounds__(64 * WA * WB, 2) void product_tile_kernel(Table a, Table b, T *out, long long ldo, int tiles_a, int tiles_b)
+__global__ __launch_bounds__(64 * WA * WB, FA * FB > 8 ? 1 : 2) void product_tile_kernel(Table a, Table b, T *out, long long ldo, int tiles_a,
+                                                                                          int tiles_b)
 {
     typedef Tiling<FA, FB, WA, WB> Tile;
-    typedef typename Tile::Lds Lds;
     extern __shared__ __align__(16) char lds_raw[];
-    Lds *stages = (Lds *)lds_raw;
+    typename Tile::Lds &lds = *(typename Tile::Lds *)lds_raw;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 31, half = lane >> 5;
     // A chiplet (every eighth workgroup) gets a connected piece of the tiles, walked in strips of eight rows of tiles: what runs
     // there together shares rows of a and of b in its L2.
@@ -216,62 +218,60 @@ __global__ __launch_bounds__(64 * WA * WB, 2) void product_tile_kernel(Table a, 
     const int rows_a = a.n - i0, rows_b = b.n - j0, n_stages = (a.nb + 7) / 8;
     const uint8_t *codes_a = a.codes + (size_t)i0 * a.nb * 16, *codes_b = b.codes + (size_t)j0 * b.nb * 16;
     const uint8_t *scales_a = a.scales + (size_t)i0 * a.sp, *scales_b = b.scales + (size_t)j0 * b.sp;
-    u32 at_codes[Tile::each], at_scales[Tile::each_words];
+    const auto row_of = [&](int row) { return (u32)(row < Tile::side_a ? min(row, rows_a - 1) : min(row - Tile::side_a, rows_b - 1)); };
+    u32 at_codes[Tile::each], at_scales[Tile::each_scales];
 #pragma unroll
-    for (int i = 0; i < Tile::each; ++i) {
-        const int row = (wave * Tile::each + i) * 8 + (lane >> 3);
-        at_codes[i] = (u32)(row < Tile::side_a ? min(row, rows_a - 1) : min(row - Tile::side_a, rows_b - 1)) * a.nb * 16;
-    }
+    for (int i = 0; i < Tile::each; ++i) at_codes[i] = row_of((wave * Tile::each + i) * 8 + (lane >> 3)) * a.nb * 16;
 #pragma unroll
-    for (int i = 0; i < Tile::each_words; ++i) {
-        const int row = (wave * Tile::each_words + i) * 64 % Tile::sides + lane;
-        at_scales[i] = (u32)(row < Tile::side_a ? min(row, rows_a - 1) : min(row - Tile::side_a, rows_b - 1)) * a.sp;
-    }
-    const auto load = [&](int stage) {
-        Lds *to = stages + (stage & 1);
+    for (int i = 0; i < Tile::each_scales; ++i) at_scales[i] = row_of((wave * Tile::each_scales + i) * 16 + (lane >> 2)) * a.sp;
+    const auto load = [&](int stage, bool with_scales) {
         const u32 block = min(8 * stage + ((lane & 7) ^ (lane >> 3)), a.nb - 1) * 16;
 #pragma unroll
         for (int i = 0; i < Tile::each; ++i) {
             const int op = wave * Tile::each + i;
-            mx_stage((op * 8 < Tile::side_a ? codes_a : codes_b) + at_codes[i] + block, &to->codes[op][0], 1);
+            mx_stage((op * 8 < Tile::side_a ? codes_a : codes_b) + at_codes[i] + block, &lds.codes[stage & 1][op][0], 1);
         }
+        if (!with_scales) return;
+        const u32 word = min(8 * stage + 4 * (lane & 3), a.sp - 4);
 #pragma unroll
-        for (int i = 0; i < Tile::each_words; ++i) {
-            const int op = wave * Tile::each_words + i, row = op * 64 % Tile::sides, word = op * 64 / Tile::sides;
-            mx_stage((row < Tile::side_a ? scales_a : scales_b) + at_scales[i] + min(8 * stage + 4 * word, a.sp - 4), &to->scales[word][row], 0);
+        for (int i = 0; i < Tile::each_scales; ++i) {
+            const int op = wave * Tile::each_scales + i;
+            mx_stage((op * 16 < Tile::side_a ? scales_a : scales_b) + at_scales[i] + word, &lds.scales[(stage >> 1) & 1][op * 16][0], 0);
         }
     };
     f32x16 acc[FA][FB] = {};
     const int wa = wave % WA * 32 * FA, wb = wave / WA * 32 * FB;
-    // where the lane's block of the first 64 coordinates is in a stage (block b ^ r % 8 of row r; 64 coordinates on: the
-    // offset ^ 32), and its scale; 32 rows further down 4096 and 128 bytes on
+    // where the lane's block of the first 64 coordinates is in a stage (64 coordinates on: the offset ^ 32; 32 rows further down:
+    // 4096 bytes on), and its row's scales
     const int code_a = (wa + r) * 128 + (half ^ (r & 7)) * 16, code_b = (Tile::side_a + wb + r) * 128 + (half ^ (r & 7)) * 16;
-    const int scale_a = (wa + r) * 4 + half, scale_b = (Tile::side_a + wb + r) * 4 + half;
-    // 64 coordinates at a time; the next operands are read while the matrix unit works on these
-    Operand oa[2][FA], ob[2][FB];
-    const auto read = [&](const Lds *now, int h, int to) {
-        const char *ca = (const char *)now->codes + (code_a ^ (32 * h)), *cb = (const char *)now->codes + (code_b ^ (32 * h));
-        const char *sa = (const char *)now->scales[h >> 1] + scale_a + 2 * (h & 1), *sb = (const char *)now->scales[h >> 1] + scale_b + 2 * (h & 1);
+    typedef u32 u32x2 __attribute__((ext_vector_type(2)));
+    i32x4 ca[2][FA], cb[2][FB];
+    u32x2 sa[2][FA], sb[2][FB];
+    const auto read_codes = [&](int stage, int h, int to) {
+        const char *pa = (const char *)lds.codes[stage & 1] + (code_a ^ (32 * h)), *pb = (const char *)lds.codes[stage & 1] + (code_b ^ (32 * h));
 #pragma unroll
-        for (int f = 0; f < FA; ++f) {
-            oa[to][f].codes = *(const i32x4 *)(ca + 32 * 128 * f);
-            oa[to][f].scale = *(const uint8_t *)(sa + 32 * 4 * f);
-        }
+        for (int f = 0; f < FA; ++f) ca[to][f] = *(const i32x4 *)(pa + 32 * 128 * f);
 #pragma unroll
-        for (int f = 0; f < FB; ++f) {
-            ob[to][f].codes = *(const i32x4 *)(cb + 32 * 128 * f);
-            ob[to][f].scale = *(const uint8_t *)(sb + 32 * 4 * f);
-        }
+        for (int f = 0; f < FB; ++f) cb[to][f] = *(const i32x4 *)(pb + 32 * 128 * f);
     };
-    const auto multiply = [&](int from) {
+    // a lane's blocks are the odd or the even ones: shifted, they are bytes 0 and 2 of two words
+    const auto read_scales = [&](int stage, int to) {
+        const u32 *from = &lds.scales[(stage >> 1) & 1][r][2 * (stage & 1)];
+#pragma unroll
+        for (int f = 0; f < FA; ++f) sa[to][f] = *(const u32x2 *)(from + 4 * (wa + 32 * f)) >> (u32)(8 * half);
+#pragma unroll
+        for (int f = 0; f < FB; ++f) sb[to][f] = *(const u32x2 *)(from + 4 * (Tile::side_a + wb + 32 * f)) >> (u32)(8 * half);
+    };
+    const auto multiply = [&](int h, int from, int scales) {
 #pragma unroll
         for (int y = 0; y < FA; ++y)
 #pragma unroll
             for (int x = 0; x < FB; ++x) {
-                const Operand &p = ob[from][x], &q = oa[from][y];
-                const i32x8 p8 = {p.codes.x, p.codes.y, p.codes.z, p.codes.w, 0, 0, 0, 0};
-                const i32x8 q8 = {q.codes.x, q.codes.y, q.codes.z, q.codes.w, 0, 0, 0, 0};
-                acc[y][x] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(p8, q8, acc[y][x], kFp4, kFp4, 0, p.scale, 0, q.scale);
+                const i32x4 p = cb[from][x], q = ca[from][y];
+                const i32x8 p8 = {p.x, p.y, p.z, p.w, 0, 0, 0, 0}, q8 = {q.x, q.y, q.z, q.w, 0, 0, 0, 0};
+                const int s = (int)sb[scales][x][h >> 1], t = (int)sa[scales][y][h >> 1];
+                acc[y][x] = h & 1 ? __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(p8, q8, acc[y][x], kFp4, kFp4, 2, s, 2, t)
+                                  : __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(p8, q8, acc[y][x], kFp4, kFp4, 0, s, 0, t);
             }
     };
     // a stage has arrived, and what was read of the one before it is in registers
@@ -280,36 +280,60 @@ __global__ __launch_bounds__(64 * WA * WB, 2) void product_tile_kernel(Table a, 
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
-    load(0);
+    load(0, true);
+    arrived();
+    if (n_stages > 1) load(1, false);
+    // Stages in pairs, without a branch (behind one, the compiler would put the matrix instructions too).  The next operands are
+    // read while the matrix unit works on these; before a stage's last piece of work the next stage has to be there, and the
+    // one after it may take this one's place.
+    const int whole = a.nb / 8;
     int stage = 0;
-    for (; 8 * stage + 8 <= a.nb; ++stage) {
-        arrived();
-        if (stage + 1 < n_stages) load(stage + 1);
-        const Lds *now = stages + (stage & 1);
-        read(now, 0, 0);
+    if (stage + 2 < whole) {
+        read_codes(0, 0, 0);
+        read_scales(0, 0);
+        for (; stage + 3 < n_stages && stage + 2 < whole; stage += 2)
 #pragma unroll
-        for (int h = 0; h < 4; ++h) {
-            if (h < 3) read(now, h + 1, (h + 1) & 1);
-            multiply(h & 1);
-            __builtin_amdgcn_sched_barrier(0);        // (reads further ahead do not fit the registers)
-        }
+            for (int odd = 0; odd < 2; ++odd) {
+#pragma unroll
+                for (int h = 0; h < 3; ++h) {
+                    read_codes(stage + odd, h + 1, (h + 1) & 1);
+                    multiply(h, h & 1, odd);
+                    __builtin_amdgcn_sched_barrier(0);        // (reads further ahead do not fit the registers)
+                }
+                arrived();
+                load(stage + odd + 2, odd == 0);
+                read_codes(stage + odd + 1, 0, 0);
+                read_scales(stage + odd + 1, 1 - odd);
+                multiply(3, 1, odd);
+                __builtin_amdgcn_sched_barrier(0);
+            }
     }
-    if (stage < n_stages) {
-        arrived();
-        Lds *now = stages + (stage & 1);
-        const int have = a.nb - 8 * stage;
+    // what is left: at most three stages and one that is not whole
+    for (; stage < n_stages; ++stage) {
+        const int have = min(a.nb - 8 * stage, 8);
         if (have & 1) {
             // the second half of the last instruction: nothing in a, and no scale of either
             for (int row = tid; row < Tile::sides; row += 64 * Tile::waves) {
-                if (row < Tile::side_a) *(i32x4 *)&now->codes[row >> 3][((row & 7) * 8 + (have ^ (row & 7))) * 4] = i32x4{0, 0, 0, 0};
-                ((uint8_t *)&now->scales[have >> 2][row])[have & 3] = 0;
+                if (row < Tile::side_a)
+                    *(i32x4 *)&lds.codes[stage & 1][row >> 3][((row & 7) * 8 + (have ^ (row & 7))) * 4] = i32x4{0, 0, 0, 0};
+                ((uint8_t *)&lds.scales[(stage >> 1) & 1][row][2 * (stage & 1)])[have] = 0;
             }
             __syncthreads();
         }
+        read_scales(stage, 0);
 #pragma unroll 1
         for (int h = 0; 2 * h < have; ++h) {
-            read(now, h, 0);
-            multiply(0);
+            read_codes(stage, h, 0);
+            multiply(0, 0, 0);
+            // the next two blocks' scales into byte 0
+#pragma unroll
+            for (int f = 0; f < FA; ++f) sa[0][f].x = h & 1 ? sa[0][f].y : sa[0][f].x >> 16;
+#pragma unroll
+            for (int f = 0; f < FB; ++f) sb[0][f].x = h & 1 ? sb[0][f].y : sb[0][f].x >> 16;
+        }
+        if (stage + 1 < n_stages) {
+            arrived();
+            if (stage + 2 < n_stages) load(stage + 2, (stage & 1) == 0);
         }
     }
     // Out through LDS, 32 rows of a wave's piece at a time, so that stores are whole rows of it.  (Straight from the registers
@@ -434,7 +458,7 @@ template <class T, int FA, int FB, int WA, int WB>
 int launch_tiles(const Table &a, const Table &b, T *out, int64_t ldo, hipStream_t st)
 {
     typedef Tiling<FA, FB, WA, WB> Tile;
-    const int stages = 2 * (int)sizeof(typename Tile::Lds), turn = Tile::waves * 32 * Tile::out_pitch * (int)sizeof(T);
+    const int stages = (int)sizeof(typename Tile::Lds), turn = Tile::waves * 32 * Tile::out_pitch * (int)sizeof(T);
     const int lds = stages > turn ? stages : turn;
     EF_HIP_CHECK(hipFuncSetAttribute((const void *)product_tile_kernel<T, FA, FB, WA, WB>, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
     const int64_t ta = (a.n + Tile::side_a - 1) / Tile::side_a, tb = (b.n + Tile::side_b - 1) / Tile::side_b;
@@ -465,7 +489,7 @@ int launch_product(const Table &a, const Table &b, T *out, int64_t ldo, hipStrea
     if (a.n <= 32) return launch_few_of<T, 2>(a, b, out, ldo, st);
     // the larger tile reads half as much from LDS and L2 per operation; the smaller one where there is less than one of those per CU
     const int64_t large = (int64_t)((a.n + 255) / 256) * ((b.n + 255) / 256);
-    return large >= 200 ? launch_tiles<T, 4, 2, 2, 4>(a, b, out, ldo, st) : launch_tiles<T, 2, 2, 2, 2>(a, b, out, ldo, st);
+    return large >= 200 ? launch_tiles<T, 4, 4, 2, 2>(a, b, out, ldo, st) : launch_tiles<T, 2, 2, 2, 2>(a, b, out, ldo, st);
 }
 
 // ---- nearest rows ----------------------------------------------------------------------------------------
