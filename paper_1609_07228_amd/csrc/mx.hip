@@ -489,7 +489,7 @@ int launch_product(const Table &a, const Table &b, T *out, int64_t ldo, hipStrea
     if (a.n <= 32) return launch_few_of<T, 2>(a, b, out, ldo, st);
     // the larger tile reads half as much from LDS and L2 per operation; the smaller one where there is less than one of those per CU
     const int64_t large = (int64_t)((a.n + 255) / 256) * ((b.n + 255) / 256);
-    return large >= 200 ? launch_tiles<T, 4, 4, 2, 2>(a, b, out, ldo, st) : launch_tiles<T, 2, 2, 2, 2>(a, b, out, ldo, st);
+    return large >= 200 ? launch_tiles<T, 4, 2, 2, 4>(a, b, out, ldo, st) : launch_tiles<T, 2, 2, 2, 2>(a, b, out, ldo, st);
 }
 
 // ---- nearest rows ----------------------------------------------------------------------------------------
