@@ -21,6 +21,9 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kFp4 = 4;                    // the operand format's number in the matrix instruction
+// Outputs larger than the L2 caches are stored past them (10^6 x 128 float32 read back: 102 -> 81 us); smaller ones are left there
+// for whoever reads them next.
+constexpr int64_t kStreamBytes = (int64_t)32 << 20;
 constexpr size_t kMaxWorkspace = (size_t)1 << 30;
 
 __host__ __device__ inline int mx_blocks(int d) { return (d + 31) >> 5; }
@@ -43,84 +46,135 @@ __device__ inline float mx_scale(u32 b)
 template <class T> __device__ inline float to_float(T x) { return (float)x; }
 template <class T> __device__ inline T from_float(float x) { return (T)x; }      // to nearest, ties to even
 
+// Eight values from or to any address that suits the element (the last ones of a row: fewer).
+template <class T>
+__device__ inline void load_eight(const T *p, int left, float (&v)[8])
+{
+    typedef T Piece __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
+    constexpr int kPer = 16 / sizeof(T);
+    if (left >= 8) {
+#pragma unroll
+        for (int i = 0; i < 8; i += kPer) {
+            const Piece x = *(const Piece *)(p + i);
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) v[i + j] = to_float(x[j]);
+        }
+    } else
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = j < left ? to_float(p[j]) : 0.0f;
+}
+// the eight values of a word of codes
+__device__ inline void mx_values(u32 word, float scale, float (&v)[8])
+{
+    const f32x2 h0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, scale, 0), h1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, scale, 1);
+    const f32x2 h2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, scale, 2), h3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, scale, 3);
+    v[0] = h0.x, v[1] = h0.y, v[2] = h1.x, v[3] = h1.y, v[4] = h2.x, v[5] = h2.y, v[6] = h3.x, v[7] = h3.y;
+}
+
+// A neighbour's value by row operations (no trip through LDS): the other lane of a pair, of a pair of pairs; the lane 4 or
+// 8 further within a row of 16, around its end.
+constexpr int kSwap1 = 0xB1, kSwap2 = 0x4E, kDown4 = 0x120 + 12, kDown8 = 0x120 + 8;
+template <int CTRL> __device__ inline u32 mx_from(u32 x) { return (u32)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true); }
+template <int CTRL> __device__ inline float mx_from(float x) { return __uint_as_float(mx_from<CTRL>(__float_as_uint(x))); }
+
 // ---- quantisation ----------------------------------------------------------------------------------------
-// Four lanes per block, eight coordinates each; a row's lanes are `group` consecutive ones (a power of two), so
-// a wave holds 64 / group rows and the row's squared length is a sum over those lanes.  Bound: HBM.
+// Four lanes per block, eight coordinates each; a row's lanes are `group` consecutive ones (a power of two, 16 at least),
+// so a wave holds 64 / group rows and the row's squared length is a sum over those lanes.  Bound: HBM.
 template <class T>
 __global__ __launch_bounds__(256) void quantise_kernel(const T *X, long long n, int d, long long ldx, int group, int nb,
                                                        int sp, uint8_t *codes, uint8_t *scales, float *norms)
 {
     const int lane = threadIdx.x & (group - 1);
-    const long long row = ((long long)blockIdx.x * 256 + threadIdx.x) / group;
+    const long long row = (long long)blockIdx.x * (256 / group) + threadIdx.x / group;
     if (row >= n) return;
     const T *x = X + row * ldx;
+    uint8_t *row_codes = codes + (size_t)row * nb * 16, *row_scales = scales + (size_t)row * sp;
     float norm = 0.0f;
     const int pieces = 4 * sp;                 // lanes past the last block write the scales' padding
     for (int p = lane; p < pieces; p += group) {
-        const int j0 = p * 8;
         float v[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = j0 + j < d ? to_float(x[j0 + j]) : 0.0f;
+        load_eight(x + p * 8, d - p * 8, v);
         u32 top = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[j]) & 0x7FFFFFFFu);
-        top = max(top, (u32)__shfl_xor((int)top, 1));
-        top = max(top, (u32)__shfl_xor((int)top, 2));
+        top = max(top, mx_from<kSwap1>(top));
+        top = max(top, mx_from<kSwap2>(top));
         const u32 e = top >> 23;
         const bool bad = e == 255;
         const u32 b = bad ? 255u : e > 2 ? e - 2 : 0u;
         const float scale = mx_scale(bad ? 127 : b);
         u32 word = 0;
-        if (!bad) {
-            word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[0], v[1], scale, 0);
-            word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[2], v[3], scale, 1);
-            word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[4], v[5], scale, 2);
-            word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[6], v[7], scale, 3);
-        }
+        word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[0], v[1], scale, 0);
+        word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[2], v[3], scale, 1);
+        word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[4], v[5], scale, 2);
+        word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[6], v[7], scale, 3);
+        if (bad) word = 0;
         const int block = p >> 2;
-        if (block < nb) *(u32 *)(codes + (size_t)row * nb * 16 + (size_t)p * 4) = word;
-        if ((p & 3) == 0) scales[(size_t)row * sp + block] = (uint8_t)(block < nb ? b : 0);
-        const f32x2 h0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, scale, 0);
-        const f32x2 h1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, scale, 1);
-        const f32x2 h2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, scale, 2);
-        const f32x2 h3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, scale, 3);
-        norm += (h0.x * h0.x + h0.y * h0.y) + (h1.x * h1.x + h1.y * h1.y) + (h2.x * h2.x + h2.y * h2.y) +
-                (h3.x * h3.x + h3.y * h3.y);
+        if (block < nb) *(u32 *)(row_codes + (size_t)p * 4) = word;
+        // four blocks' scales as a word
+        u32 four = block < nb ? b : 0;
+        four |= mx_from<kDown4>(four) << 8;
+        four |= mx_from<kDown8>(four) << 16;
+        if ((p & 15) == 0) *(u32 *)(row_scales + block) = four;
+        mx_values(word, scale, v);
+        norm += (v[0] * v[0] + v[1] * v[1]) + (v[2] * v[2] + v[3] * v[3]) + (v[4] * v[4] + v[5] * v[5]) + (v[6] * v[6] + v[7] * v[7]);
         if (bad) norm = __uint_as_float(0x7FC00000u);
     }
-    for (int o = 1; o < group; o <<= 1) norm += __shfl_xor(norm, o);
+    norm += mx_from<kSwap1>(norm);
+    norm += mx_from<kSwap2>(norm);
+    norm += mx_from<kDown4>(norm);
+    norm += mx_from<kDown8>(norm);
+    for (int o = 16; o < group; o <<= 1) norm += __shfl_xor(norm, o);
     if (lane == 0) norms[row] = norm;
 }
 
 // ---- rows by id ------------------------------------------------------------------------------------------
-// A lane per eight coordinates of an output row: one word of codes in, eight values out.  Bound: HBM writes.
-template <class T>
-__global__ __launch_bounds__(256) void rows_kernel(Table t, int d, const int *ids, long long m, int lanes, float factor,
-                                                   T *out)
+// A lane per 16 bytes of an output row (4 or 8 coordinates: neighbouring lanes' stores touch), `group` lanes (a power of two)
+// per row and kRows rows per lane, so that as many chains of id, codes, store run side by side.  Bound: HBM writes.
+constexpr int kRows = 4;
+template <class T, bool PAST_CACHE>
+__global__ __launch_bounds__(256) void rows_kernel(Table t, int d, const int *ids, long long m, int group, float factor, T *out)
 {
-    const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
-    const long long i = at / lanes;
-    const int p = (int)(at - i * lanes);
-    if (i >= m) return;
-    const int id = ids ? ids[i] : (int)i;
-    const int j0 = p * 8;
-    float v[8] = {};
-    if (id >= 0 && id < t.n) {
-        const u32 word = *(const u32 *)(t.codes + (size_t)id * t.nb * 16 + (size_t)p * 4);
-        const float scale = mx_scale(t.scales[(size_t)id * t.sp + (p >> 2)]);
-        const f32x2 h0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, 1.0f, 0);
-        const f32x2 h1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, 1.0f, 1);
-        const f32x2 h2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, 1.0f, 2);
-        const f32x2 h3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, 1.0f, 3);
-        v[0] = h0.x * scale, v[1] = h0.y * scale, v[2] = h1.x * scale, v[3] = h1.y * scale;
-        v[4] = h2.x * scale, v[5] = h2.y * scale, v[6] = h3.x * scale, v[7] = h3.y * scale;
+    constexpr int kPer = 16 / sizeof(T);
+    typedef T Piece __attribute__((ext_vector_type(kPer), aligned(sizeof(T))));
+    const int lane = threadIdx.x & (group - 1), per = 256 / group;
+    const long long first = (long long)blockIdx.x * (per * kRows) + threadIdx.x / group;
+    int id[kRows];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] *= factor;
+    for (int i = 0; i < kRows; ++i) {
+        const long long row = min(first + (long long)i * per, m - 1);
+        id[i] = ids ? ids[row] : (int)row;
     }
-    T *o = out + (size_t)i * d + j0;
+    for (int p = lane; p * kPer < d; p += group) {
+        u32 word[kRows], b[kRows];
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-        if (j0 + j < d) o[j] = from_float<T>(v[j]);
+        for (int i = 0; i < kRows; ++i) {
+            word[i] = 0, b[i] = 256;                   // (an empty slot)
+            if (id[i] >= 0 && id[i] < t.n) {
+                word[i] = *(const u32 *)(t.codes + (size_t)id[i] * t.nb * 16 + (size_t)(p * kPer / 8) * 4);
+                b[i] = t.scales[(size_t)id[i] * t.sp + p * kPer / 32];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            const long long row = first + (long long)i * per;
+            float v[8];
+            mx_values(kPer == 4 ? word[i] >> (16 * (p & 1)) : word[i], 1.0f, v);
+            const float scale = mx_scale(b[i] & 255);
+            Piece x;
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) x[j] = from_float<T>(b[i] > 255 ? 0.0f : v[j] * scale * factor);
+            if (row >= m) continue;
+            T *o = out + (size_t)row * d + p * kPer;
+            if (d - p * kPer >= kPer) {
+                if (PAST_CACHE) __builtin_nontemporal_store(x, (Piece *)o);
+                else *(Piece *)o = x;
+            } else
+#pragma unroll
+                for (int j = 0; j < kPer; ++j)
+                    if (p * kPer + j < d) o[j] = x[j];
+        }
+    }
 }
 
 // ---- matrix instruction --------------------------------------------------------------------------------------
@@ -1294,9 +1348,9 @@ extern "C" int efanna_mx_quantise(const void *X, int32_t dtype, int64_t n, int32
     if (!X || !norms || !aligned_for(X, dtype) || ((uintptr_t)norms & 3)) return EFANNA_EINVAL;
     hipStream_t st = (hipStream_t)stream;
     const int nb = mx_blocks(d), sp = mx_scale_pitch(d);
-    int group = 4;
+    int group = 16;
     while (group < 64 && group < 4 * sp) group <<= 1;
-    const int64_t blocks = (n * group + 255) / 256;
+    const int64_t blocks = (n + 256 / group - 1) / (256 / group);
     EF_MX_DTYPE(dtype, T, (quantise_kernel<T><<<(unsigned)blocks, 256, 0, st>>>((const T *)X, n, d, ldx, group, nb, sp, codes, scales, norms)));
     EF_HIP_CHECK(hipGetLastError());
     return EFANNA_OK;
@@ -1310,10 +1364,15 @@ extern "C" int efanna_mx_rows(const uint8_t *codes, const uint8_t *scales, int64
     if (!out || !aligned_for(out, dtype) || ((uintptr_t)ids & 3)) return EFANNA_EINVAL;
     hipStream_t st = (hipStream_t)stream;
     const Table t = {codes, scales, nullptr, (int)n, mx_blocks(d), mx_scale_pitch(d)};
-    const int lanes = (d + 7) / 8;
-    const int64_t blocks = (m * lanes + 255) / 256;
-    if (blocks > 2147483647LL) return EFANNA_EUNSUPPORTED;
-    EF_MX_DTYPE(dtype, T, (rows_kernel<T><<<(unsigned)blocks, 256, 0, st>>>(t, d, ids, m, lanes, factor, (T *)out)));
+    const int per = dtype == EFANNA_F32 ? 4 : 8;
+    const bool past_cache = m * d * (16 / per) > kStreamBytes;
+    int group = 1;
+    while (group < 64 && group * per < d) group <<= 1;
+    const int64_t rows = kRows * (256 / group), blocks = (m + rows - 1) / rows;
+    EF_MX_DTYPE(dtype, T, {
+        if (past_cache) rows_kernel<T, true><<<(unsigned)blocks, 256, 0, st>>>(t, d, ids, m, group, factor, (T *)out);
+        else rows_kernel<T, false><<<(unsigned)blocks, 256, 0, st>>>(t, d, ids, m, group, factor, (T *)out);
+    });
     EF_HIP_CHECK(hipGetLastError());
     return EFANNA_OK;
 }
