@@ -26,6 +26,11 @@ constexpr int kFp4 = 4;                    // the operand format's number in the
 constexpr int64_t kStreamBytes = (int64_t)32 << 20;
 constexpr size_t kMaxWorkspace = (size_t)1 << 30;
 
+// (64 KiB and less need no leave, and asking for it takes a microsecond)
+inline hipError_t allow_lds(const void *kernel, int bytes)
+{
+    return bytes > 65536 ? hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) : hipSuccess;
+}
 __host__ __device__ inline int mx_blocks(int d) { return (d + 31) >> 5; }
 __host__ __device__ inline int mx_scale_pitch(int d) { return (mx_blocks(d) + 3) & ~3; }
 inline size_t align_up(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -514,7 +519,7 @@ int launch_tiles(const Table &a, const Table &b, T *out, int64_t ldo, hipStream_
     typedef Tiling<FA, FB, WA, WB> Tile;
     const int stages = (int)sizeof(typename Tile::Lds), turn = Tile::waves * 32 * Tile::out_pitch * (int)sizeof(T);
     const int lds = stages > turn ? stages : turn;
-    EF_HIP_CHECK(hipFuncSetAttribute((const void *)product_tile_kernel<T, FA, FB, WA, WB>, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+    EF_HIP_CHECK(allow_lds((const void *)product_tile_kernel<T, FA, FB, WA, WB>, lds));
     const int64_t ta = (a.n + Tile::side_a - 1) / Tile::side_a, tb = (b.n + Tile::side_b - 1) / Tile::side_b;
     if (ta * tb > 2147483647LL) return EFANNA_EUNSUPPORTED;
     product_tile_kernel<T, FA, FB, WA, WB><<<(unsigned)(ta * tb), 64 * Tile::waves, lds, st>>>(a, b, out, ldo, (int)ta, (int)tb);
@@ -524,7 +529,7 @@ template <class T, int M, int S, int WAVES>
 int launch_few(const Table &a, const Table &b, T *out, int64_t ldo, hipStream_t st)
 {
     const int stage = WAVES * (int)sizeof(FewLds<S>), join = (WAVES - 1) * M * 4 * 64 * 16, lds = stage > join ? stage : join;
-    EF_HIP_CHECK(hipFuncSetAttribute((const void *)product_few_kernel<T, M, S, WAVES>, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+    EF_HIP_CHECK(allow_lds((const void *)product_few_kernel<T, M, S, WAVES>, lds));
     product_few_kernel<T, M, S, WAVES><<<(unsigned)((b.n + 63) / 64), 64 * WAVES, lds, st>>>(a, b, out, ldo);
     return EFANNA_OK;
 }
@@ -1254,7 +1259,7 @@ template <int WAVES, int S>
 int launch_pick_of(const Scan &a, int k, int64_t first_self, int32_t *ids, float *dists, hipStream_t st)
 {
     const int kk = k + (first_self >= 0 ? 1 : 0), lds = WAVES * ((2 * kk + kListRoom) * 8 + (int)sizeof(ScoreLds<S>));
-    EF_HIP_CHECK(hipFuncSetAttribute((const void *)pick_kernel<WAVES, S>, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+    EF_HIP_CHECK(allow_lds((const void *)pick_kernel<WAVES, S>, lds));
     const int blocks = WAVES > 1 ? a.nq : (a.nq + 127) & ~127;
     pick_kernel<WAVES, S><<<(unsigned)blocks, 64 * WAVES, lds, st>>>(a, k, first_self, ids, dists);
     return EFANNA_OK;
@@ -1271,7 +1276,7 @@ template <int KS, int QF>
 int launch_wide(Scan a, hipStream_t st)
 {
     const int lds = 2 * (int)sizeof(StageLds<KS == 1 ? kStage : KS == 2 ? kStage / 2 : KS <= 4 ? kStage / 4 : kStage / 8, KS>);
-    EF_HIP_CHECK(hipFuncSetAttribute((const void *)scan_wide_kernel<KS, QF>, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+    EF_HIP_CHECK(allow_lds((const void *)scan_wide_kernel<KS, QF>, lds));
     a.q_parts = (a.nq + 128 * QF - 1) / (128 * QF);
     // supers per workgroup: enough for its queries' loads to be little next to its rows', few enough to fill the CUs (two workgroups
     // of one step each, one of more) twice
@@ -1288,7 +1293,7 @@ template <int KS, int QF>
 int launch_narrow(const Scan &a, hipStream_t st)
 {
     const int lds = 4 * (int)sizeof(StageLds<KS == 1 ? 16 : KS == 2 ? 8 : KS <= 4 ? 4 : 2, KS>);
-    EF_HIP_CHECK(hipFuncSetAttribute((const void *)scan_narrow_kernel<KS, QF>, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+    EF_HIP_CHECK(allow_lds((const void *)scan_narrow_kernel<KS, QF>, lds));
     scan_narrow_kernel<KS, QF><<<dim3((unsigned)a.supers, (unsigned)((a.nq + 16 * QF - 1) / (16 * QF))), 256, lds, st>>>(a);
     return EFANNA_OK;
 }
