@@ -348,7 +348,7 @@ int efanna_mx_product(const uint8_t *a_codes, const uint8_t *a_scales, int64_t m
  *        +inf where there are fewer than k.
  * Limits: 1 <= k <= EFANNA_MAX_K.  The workspace holds at most about 1 GiB (more queries take several
  * passes; at least 256 queries go together, which beyond 15 * 10^6 rows takes more). */
-size_t efanna_mx_nearest_workspace_bytes(int64_t n, int64_t nq, int32_t k);
+size_t efanna_mx_nearest_workspace_bytes(int64_t n, int32_t d, int64_t nq, int32_t k);
 
 int efanna_mx_nearest(const uint8_t *codes, const uint8_t *scales, const float *norms, int64_t n, int32_t d,
                       const uint8_t *q_codes, const uint8_t *q_scales, const float *q_norms, int64_t nq,

@@ -1233,12 +1233,13 @@ struct NearestShape {
     int tiles, supers, chunk;      // tiles per block, supers of the table, queries per pass
     size_t gmin_bytes, bytes;
 };
-inline NearestShape nearest_shape(int64_t n, int64_t nq, int k)
+inline NearestShape nearest_shape(int64_t n, int d, int64_t nq, int k)
 {
     NearestShape s;
     // Group size: the scan writes a value per group, the pick reads the rows of k groups.
     s.tiles = 4;
-    while (s.tiles < 32 && (int64_t)s.tiles * s.tiles * 480 * (k + 1) <= n) s.tiles *= 2;
+    const int row = mx_blocks(d) > 4 ? mx_blocks(d) : 4;
+    while (s.tiles < 32 && (int64_t)s.tiles * s.tiles * 120 * row * (k + 1) <= n) s.tiles *= 2;
     const int64_t super_rows = 64 * s.tiles;
     s.supers = (int)((n + super_rows - 1) / super_rows);
     const size_t per16 = (size_t)s.supers * 17 * 16 * sizeof(float);     // 16 queries: groups and supers
@@ -1410,10 +1411,10 @@ extern "C" int efanna_mx_product(const uint8_t *a_codes, const uint8_t *a_scales
     return EFANNA_OK;
 }
 
-extern "C" size_t efanna_mx_nearest_workspace_bytes(int64_t n, int64_t nq, int32_t k)
+extern "C" size_t efanna_mx_nearest_workspace_bytes(int64_t n, int32_t d, int64_t nq, int32_t k)
 {
-    if (n < 0 || nq < 0 || n > kMaxRows || nq > kMaxRows || k < 1 || k > EFANNA_MAX_K) return 0;
-    return nearest_shape(n, nq, k).bytes;
+    if (d < 1 || d > EFANNA_MX_MAX_D || n < 0 || nq < 0 || n > kMaxRows || nq > kMaxRows || k < 1 || k > EFANNA_MAX_K) return 0;
+    return nearest_shape(n, d, nq, k).bytes;
 }
 
 extern "C" int efanna_mx_nearest(const uint8_t *codes, const uint8_t *scales, const float *norms, int64_t n, int32_t d,
@@ -1427,7 +1428,7 @@ extern "C" int efanna_mx_nearest(const uint8_t *codes, const uint8_t *scales, co
     if ((n > 0 && !norms) || !q_norms || !ids || !dists || ((uintptr_t)norms & 15) || ((uintptr_t)q_norms & 3) ||
         ((uintptr_t)ids & 3) || ((uintptr_t)dists & 3))
         return EFANNA_EINVAL;
-    const NearestShape sh = nearest_shape(n, nq, k);
+    const NearestShape sh = nearest_shape(n, d, nq, k);
     if (!ws || ((uintptr_t)ws & 255) || ws_bytes < sh.bytes) return EFANNA_EWORKSPACE;
     hipStream_t st = (hipStream_t)stream;
     const int nb = mx_blocks(d), sp = mx_scale_pitch(d);

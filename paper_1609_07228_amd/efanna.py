@@ -81,7 +81,7 @@ def lib():
         L.efanna_mx_product.restype = C.c_int
         L.efanna_mx_product.argtypes = [vp, vp, i64, vp, vp, i64, i32, i32, vp, i64, vp]
         L.efanna_mx_nearest_workspace_bytes.restype = sz
-        L.efanna_mx_nearest_workspace_bytes.argtypes = [i64, i64, i32]
+        L.efanna_mx_nearest_workspace_bytes.argtypes = [i64, i32, i64, i32]
         L.efanna_mx_nearest.restype = C.c_int
         L.efanna_mx_nearest.argtypes = [vp, vp, vp, i64, i32, vp, vp, vp, i64, i32, i64, vp, vp, vp, sz, vp]
         _lib = L
@@ -406,7 +406,7 @@ def efanna_mx_nearest(table: MxTable, queries: MxTable, k: int, first_self: int 
     device = table.codes.device
     ids = torch.empty((nq, max(k, 0)), dtype=torch.int32, device=device)
     dists = torch.empty((nq, max(k, 0)), dtype=torch.float32, device=device)
-    ws = _workspace(lib().efanna_mx_nearest_workspace_bytes(n, nq, k), device) if workspace is None else workspace
+    ws = _workspace(lib().efanna_mx_nearest_workspace_bytes(n, table.d, nq, k), device) if workspace is None else workspace
     _check(lib().efanna_mx_nearest(table.codes.data_ptr(), table.scales.data_ptr(), table.norms.data_ptr(), n, table.d,
                                    queries.codes.data_ptr(), queries.scales.data_ptr(), queries.norms.data_ptr(), nq, k,
                                    int(first_self), ids.data_ptr(), dists.data_ptr(), ws.data_ptr(), ws.numel(), _stream()),

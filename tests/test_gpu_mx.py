@@ -418,7 +418,7 @@ def test_nearest_in_several_passes_and_on_a_given_workspace(ef):
     t, X = table(ef, x)
     y = vectors(rng, nq, 16, "grid")
     q, Q = table(ef, y)
-    need = ef.lib().efanna_mx_nearest_workspace_bytes(n, nq, 6)
+    need = ef.lib().efanna_mx_nearest_workspace_bytes(n, 16, nq, 6)
     ws = torch.full((need + 512,), 0xA5, dtype=torch.uint8, device="cuda")
     ids, dists = ef.efanna_mx_nearest(t, q, 6, workspace=ws[:need])
     assert (host(ws[need:]) == 0xA5).all()

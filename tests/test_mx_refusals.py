@@ -64,7 +64,7 @@ def test_product(efanna):
 
 def test_nearest(efanna):
     L = efanna.lib()
-    need = L.efanna_mx_nearest_workspace_bytes(1000, 20, 5)
+    need = L.efanna_mx_nearest_workspace_bytes(1000, 64, 20, 5)
     assert need > 0
     ok = dict(c=ONE, s=ONE, x=ONE, n=1000, d=64, qc=ONE, qs=ONE, qx=ONE, nq=20, k=5, first_self=-1, ids=ONE, dists=ONE,
               ws=ONE, ws_bytes=need, stream=None)
@@ -83,12 +83,12 @@ def test_nearest(efanna):
 
 def test_workspace_sizes(efanna):
     need = efanna.lib().efanna_mx_nearest_workspace_bytes
-    assert need(-1, 1, 1) == need(1, -1, 1) == need(1, 1, 0) == need(1, 1, 129) == 0
-    assert need(2 ** 31, 1, 1) == 0
-    assert 0 < need(0, 0, 1) <= 4096
-    assert need(1000, 1, 1) <= need(100_000, 1, 1) <= need(100_000, 1000, 1)
-    for n, nq, k in ((1_000_000, 10_000, 10), (1_000_000, 1_000_000, 10), (4_000_000, 4_000_000, 100)):
-        assert need(n, nq, k) <= (1 << 30) + (1 << 20)      # further queries take further passes
+    assert need(-1, 64, 1, 1) == need(1, 64, -1, 1) == need(1, 64, 1, 0) == need(1, 64, 1, 129) == 0
+    assert need(2 ** 31, 64, 1, 1) == need(1, 0, 1, 1) == need(1, 65537, 1, 1) == 0
+    assert 0 < need(0, 64, 0, 1) <= 4096
+    assert need(1000, 64, 1, 1) <= need(100_000, 64, 1, 1) <= need(100_000, 64, 1000, 1)
+    for n, d, nq, k in ((1_000_000, 128, 10_000, 10), (1_000_000, 960, 1_000_000, 10), (4_000_000, 96, 4_000_000, 100)):
+        assert need(n, d, nq, k) <= (1 << 30) + (1 << 20)      # further queries take further passes
 
 
 def test_binding_checks_types_shapes_and_devices(efanna):
