@@ -922,16 +922,22 @@ __global__ __launch_bounds__(256, 2) void scan_narrow_kernel(Scan a)
     }
 }
 
-// The `want`-th smallest of a wave's 64 * R words (want <= 64 * R), bit by bit; `less` of them are smaller.
+// A word that separates the `want` smallest of a wave's 64 * R words (want <= 64 * R) from the others, bit by bit: exactly
+// `want` of them do not exceed it (sharp), or it is the want-th smallest, which others equal; `less` are smaller then.
 template <int R>
-__device__ inline u32 wave_nth(const u32 (&v)[R], int want, int &less)
+__device__ inline u32 wave_nth(const u32 (&v)[R], int want, int &less, bool &sharp)
 {
     u32 t = 0;
     less = 0;
+    sharp = false;
     for (u32 bit = 0x80000000u; bit != 0; bit >>= 1) {
-        int n = 0;                         // words whose leading bits are t's with this bit 0: those below t + bit, less the smaller ones
+        int n = 0;
 #pragma unroll
         for (int i = 0; i < R; ++i) n += __popcll(__ballot(v[i] < t + bit));
+        if (n == want) {
+            sharp = true;
+            return t + bit - 1;
+        }
         if (n < want) {
             t += bit;
             less = n;
@@ -996,17 +1002,16 @@ struct KeyList {
             word[i] = (u32)(mine[i] >> 32);
         }
         __builtin_amdgcn_wave_barrier();
-        int less, equal = 0;
-        const u32 w = wave_nth(word, want, less);
-#pragma unroll
-        for (int i = 0; i < ROUNDS; ++i) equal += __popcll(__ballot(word[i] == w));
+        int less;
+        bool sharp;
+        const u32 w = wave_nth(word, want, less, sharp);
         u32 last = ~0u;
-        if (less + equal > want) {
+        if (!sharp) {
             u32 index[ROUNDS];
 #pragma unroll
             for (int i = 0; i < ROUNDS; ++i) index[i] = word[i] == w ? (u32)mine[i] : ~0u;
             int unused;
-            last = wave_nth(index, want - less, unused);
+            last = wave_nth(index, want - less, unused, sharp);
         }
         limit = ((u64)w << 32) | last;
         count = 0;
@@ -1051,12 +1056,13 @@ __device__ inline void choose(KeyList &list, int m, int lane, Word word, Name na
             // the want-th of the words, or of the lanes' smallest words: at least want of the words do not exceed either, and
             // where want is far below 64 few more do
             int unused;
+            bool sharp;
             if (list.want <= 32) {
                 u32 low[1] = {v[0]};
 #pragma unroll
                 for (int c = 1; c < 8; ++c) low[0] = min(low[0], v[c]);
-                bound = wave_nth(low, list.want, unused);
-            } else bound = wave_nth(v, list.want, unused);
+                bound = wave_nth(low, list.want, unused, sharp);
+            } else bound = wave_nth(v, list.want, unused, sharp);
         }
 #pragma unroll
         for (int c = 0; c < 8; ++c) {
