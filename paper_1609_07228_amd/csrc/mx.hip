@@ -341,8 +341,11 @@ __global__ __launch_bounds__(64 * WA * WB, FA * FB > 8 ? 1 : 2) void product_til
         asm volatile("" ::: "memory");
     };
     load(0, true);
-    arrived();
     if (n_stages > 1) load(1, false);
+    if (n_stages > 1) wait_loads<Tile::each>();      // (the second stage may still be out)
+    else wait_loads<0>();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
     // Stages in pairs, without a branch (behind one, the compiler would put the matrix instructions too).  The next operands are
     // read while the matrix unit works on these; before a stage's last piece of work the next stage has to be there, and the
     // one after it may take this one's place.
@@ -842,7 +845,12 @@ __global__ __launch_bounds__(512, KS == 1 ? 4 : 2) void scan_wide_kernel(Scan a)
             const int block = (done >> log_tiles) - 1;
 #pragma unroll
             for (int f = 0; f < QF; ++f) {
-                if (q0 + 16 * f < a.nq) a.gmin[((size_t)(q0 / 16 + f) * a.supers * 4 + block) * 64 + lane] = best[f];
+                if (q0 + 16 * f < a.nq) {
+                    float *to = &a.gmin[((size_t)(q0 / 16 + f) * a.supers * 4 + block) * 64 + lane];
+                    // (past the caches where there are many: 10^4 queries of 10^6 rows 755 -> 731 us)
+                    if (QF == 8) __builtin_nontemporal_store(best[f], to);
+                    else *to = best[f];
+                }
                 best_s[f] = mx_min(best_s[f], best[f]);
                 best[f] = __builtin_inff();
             }
