@@ -894,25 +894,30 @@ __global__ __launch_bounds__(256, 2) void scan_narrow_kernel(Scan a)
         stage->template load<1>(a.t, 0, lane, row_of);
         if (tile0 == 0) q.load(a, q0, r, g);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        const auto pass = [&](auto careful_) {
+        const auto pass = [&](auto careful_, int tile) {
             constexpr bool kCareful = decltype(careful_)::value;
-#pragma unroll(kCareful ? 1 : KS <= 2 ? 4 : 1)
-            for (int tile = 0; tile < TS; ++tile) {
-                const int left = a.t.n - mx_tile_row(row0, a.tiles, min(tile0 + tile, a.tiles - 1), 4 * g);
-                const f32x4 start = mx_start<kCareful>(stage, tile, g, left);
-                StagedRows<Lds, KS> x = {stage, tile, r, at_lane, g, b_last, false};
-                if (kCareful) x.out = !mx_takes_part(stage->norms[tile][r]);
-                f32x4 acc[QF];
-                q.tile(x, start, acc);
+            const int left = a.t.n - mx_tile_row(row0, a.tiles, min(tile0 + tile, a.tiles - 1), 4 * g);
+            const f32x4 start = mx_start<kCareful>(stage, tile, g, left);
+            StagedRows<Lds, KS> x = {stage, tile, r, at_lane, g, b_last, false};
+            if (kCareful) x.out = !mx_takes_part(stage->norms[tile][r]);
+            f32x4 acc[QF];
+            q.tile(x, start, acc);
 #pragma unroll
-                for (int f = 0; f < QF; ++f) {
-                    best[f] = mx_min(mx_min(best[f], acc[f][0]), acc[f][1]);
-                    best[f] = mx_min(mx_min(best[f], acc[f][2]), acc[f][3]);
-                }
+            for (int f = 0; f < QF; ++f) {
+                best[f] = mx_min(mx_min(best[f], acc[f][0]), acc[f][1]);
+                best[f] = mx_min(mx_min(best[f], acc[f][2]), acc[f][3]);
             }
         };
-        if (stage->odd(lane) || row0 + 16 * a.tiles > a.t.n) pass(std::true_type());
-        else pass(std::false_type());
+        if (stage->odd(lane) || row0 + 16 * a.tiles > a.t.n) {
+#pragma unroll 1
+            for (int tile = 0; tile < TS; ++tile) pass(std::true_type(), tile);
+        } else if constexpr (KS <= 2) {
+#pragma unroll 4
+            for (int tile = 0; tile < TS; ++tile) pass(std::false_type(), tile);
+        } else {
+#pragma unroll 1
+            for (int tile = 0; tile < TS; ++tile) pass(std::false_type(), tile);
+        }
     }
 #pragma unroll
     for (int f = 0; f < QF; ++f) {
