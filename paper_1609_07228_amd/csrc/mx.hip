@@ -241,14 +241,14 @@ template <int N> __device__ inline void wait_loads() { asm volatile("s_waitcnt v
 // WA x WB waves share a tile of a's rows by b's rows, FA x FB instructions of 32 x 32 x 64 each.  A stage is 256
 // coordinates of both, whole lines of 128 bytes (half lines cost the loads as much each), and the scales of 512 coordinates
 // with every other one; while one is computed the next is on its way into LDS.  A load of codes brings 8 rows; the blocks of row
-// r lie in the order b ^ r % 8, so that blocks b of eight rows, which are read together, are in different banks.
+// r lie in the order b ^ (r / 2) % 8, so that blocks b of 16 rows, which are read together, are in different ones of the 64 banks.
 // A wave reads (FA + FB) KiB from LDS for FA * FB instructions of 32 cycles; with four waves of 4 x 4 LDS is busy for 0.6 of
 // them, with eight of 4 x 2 for 0.9.
 template <int FA, int FB, int WA, int WB>
 struct Tiling {
     static constexpr int waves = WA * WB, side_a = 32 * FA * WA, side_b = 32 * FB * WB, sides = side_a + side_b;
     static constexpr int each = sides / 8 / waves, each_scales = sides / 16 / waves;      // loads of a wave
-    static_assert(sides % (16 * waves) == 0, "every wave loads as much");
+    static_assert(sides % (16 * waves) == 0, "every wave loads as much, an even number of groups of 8 rows");
     struct Lds {
         u32 codes[2][sides / 8][256];       // a's rows, then b's
         u32 scales[2][sides][4];
@@ -285,11 +285,13 @@ __global__ __launch_bounds__(64 * WA * WB, FA * FB > 8 ? 1 : 2) void product_til
 #pragma unroll
     for (int i = 0; i < Tile::each_scales; ++i) at_scales[i] = row_of((wave * Tile::each_scales + i) * 16 + (lane >> 2)) * a.sp;
     const auto load = [&](int stage, bool with_scales) {
-        const u32 block = min(8 * stage + ((lane & 7) ^ (lane >> 3)), a.nb - 1) * 16;
+        u32 block[2];          // of even and of odd groups of 8 rows
+#pragma unroll
+        for (int i = 0; i < 2; ++i) block[i] = min(8 * stage + ((lane & 7) ^ (4 * i + (lane >> 4))), a.nb - 1) * 16;
 #pragma unroll
         for (int i = 0; i < Tile::each; ++i) {
             const int op = wave * Tile::each + i;
-            mx_stage((op * 8 < Tile::side_a ? codes_a : codes_b) + at_codes[i] + block, &lds.codes[stage & 1][op][0], 1);
+            mx_stage((op * 8 < Tile::side_a ? codes_a : codes_b) + at_codes[i] + block[i & 1], &lds.codes[stage & 1][op][0], 1);
         }
         if (!with_scales) return;
         const u32 word = min(8 * stage + 4 * (lane & 3), a.sp - 4);
@@ -303,7 +305,7 @@ __global__ __launch_bounds__(64 * WA * WB, FA * FB > 8 ? 1 : 2) void product_til
     const int wa = wave % WA * 32 * FA, wb = wave / WA * 32 * FB;
     // where the lane's block of the first 64 coordinates is in a stage (64 coordinates on: the offset ^ 32; 32 rows further down:
     // 4096 bytes on), and its row's scales
-    const int code_a = (wa + r) * 128 + (half ^ (r & 7)) * 16, code_b = (Tile::side_a + wb + r) * 128 + (half ^ (r & 7)) * 16;
+    const int code_a = (wa + r) * 128 + (half ^ ((r >> 1) & 7)) * 16, code_b = code_a + (Tile::side_a + wb - wa) * 128;
     typedef u32 u32x2 __attribute__((ext_vector_type(2)));
     i32x4 ca[2][FA], cb[2][FB];
     u32x2 sa[2][FA], sb[2][FB];
@@ -378,7 +380,7 @@ __global__ __launch_bounds__(64 * WA * WB, FA * FB > 8 ? 1 : 2) void product_til
             // the second half of the last instruction: nothing in a, and no scale of either
             for (int row = tid; row < Tile::sides; row += 64 * Tile::waves) {
                 if (row < Tile::side_a)
-                    *(i32x4 *)&lds.codes[stage & 1][row >> 3][((row & 7) * 8 + (have ^ (row & 7))) * 4] = i32x4{0, 0, 0, 0};
+                    *(i32x4 *)&lds.codes[stage & 1][row >> 3][((row & 7) * 8 + (have ^ ((row >> 1) & 7))) * 4] = i32x4{0, 0, 0, 0};
                 ((uint8_t *)&lds.scales[(stage >> 1) & 1][row][2 * (stage & 1)])[have] = 0;
             }
             __syncthreads();
