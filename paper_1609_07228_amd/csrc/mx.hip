@@ -1056,96 +1056,82 @@ struct KeyList {
     }
 };
 
-// The list's `want` smallest of m keys (word(i), name(i)); a word of kOrderInf and more is nothing.
+// Takes the keys (word(i), name(i)) of i0 <= i < min(m, i0 + 64 * C), one at least, into the list; a word of kOrderInf and more is nothing.
+template <int C, class Word, class Name>
+__device__ inline void choose_part(KeyList &list, int i0, int m, int lane, Word word, Name name)
+{
+    u32 v[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) v[c] = word(min(i0 + c * 64 + lane, m - 1));      // (no load waits behind a condition)
+#pragma unroll
+    for (int c = 0; c < C; ++c) v[c] = i0 + c * 64 + lane < m ? v[c] : ~0u;
+    u32 bound = ~0u;
+    if (list.limit == ~0ULL && m - i0 > list.want) {
+        // the want-th of the words, or of the lanes' smallest words: at least want of the words do not exceed either, and
+        // where want is far below 64 few more do
+        int unused;
+        bool sharp;
+        if (list.want <= 32) {
+            u32 low[1] = {v[0]};
+#pragma unroll
+            for (int c = 1; c < C; ++c) low[0] = min(low[0], v[c]);
+            bound = wave_nth(low, list.want, unused, sharp);
+        } else if (list.want < 64 * C) bound = wave_nth(v, list.want, unused, sharp);
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const bool take = v[c] < kOrderInf && v[c] <= bound;
+        if (__any(take)) list.push(((u64)v[c] << 32) | (u32)(take ? name(i0 + c * 64 + lane) : 0), take, lane);
+    }
+    list.cut(lane);
+}
+// The list's `want` smallest of m keys.  (Eight loads per lane at a time where there is so much; fewer cost fewer instructions.)
 template <class Word, class Name>
 __device__ inline void choose(KeyList &list, int m, int lane, Word word, Name name)
 {
-    for (int i0 = 0; i0 < m; i0 += 512) {
-        u32 v[8];
-#pragma unroll
-        for (int c = 0; c < 8; ++c) v[c] = word(min(i0 + c * 64 + lane, m - 1));      // (no load waits behind a condition)
-#pragma unroll
-        for (int c = 0; c < 8; ++c) v[c] = i0 + c * 64 + lane < m ? v[c] : ~0u;
-        u32 bound = ~0u;
-        if (list.limit == ~0ULL && m - i0 > list.want) {
-            // the want-th of the words, or of the lanes' smallest words: at least want of the words do not exceed either, and
-            // where want is far below 64 few more do
-            int unused;
-            bool sharp;
-            if (list.want <= 32) {
-                u32 low[1] = {v[0]};
-#pragma unroll
-                for (int c = 1; c < 8; ++c) low[0] = min(low[0], v[c]);
-                bound = wave_nth(low, list.want, unused, sharp);
-            } else bound = wave_nth(v, list.want, unused, sharp);
-        }
-#pragma unroll
-        for (int c = 0; c < 8; ++c) {
-            const bool take = v[c] < kOrderInf && v[c] <= bound;
-            if (__any(take)) list.push(((u64)v[c] << 32) | (u32)(take ? name(i0 + c * 64 + lane) : 0), take, lane);
-        }
-        list.cut(lane);
-    }
+    if (m == 0) return;              // (a part reads one key at least)
+    if (m <= 128) return choose_part<2>(list, 0, m, lane, word, name);
+    if (m <= 256) return choose_part<4>(list, 0, m, lane, word, name);
+    for (int i0 = 0; i0 < m; i0 += 512) choose_part<8>(list, i0, m, lane, word, name);
 }
 
-// u of the 16 rows from row0 (the same for all lanes) on, four tiles side by side, S steps at a time through the wave's own
-// piece of LDS.  row0 is a row of the table; rows past its end have u = inf.
+// u of 64 rows, a lane each: lane (g, r) asks for row 4 g + r % 4 of tile r / 4, which begins at row0[r / 4] (the same for all lanes)
+// and is a row of the table.  Every column of the instruction is the query, so that of the four values that a lane gets of each tile
+// it needs one, and start values elsewhere do not matter: all of a lane's are its row's norm.  S steps at a time pass through the
+// wave's own piece of LDS.
 template <int S>
 struct ScoreLds {
     u32 codes[4 * S][256];
     u32 scales[S][4][16];
 };
 template <int S>
-__device__ inline void score_tiles(const Table &t, const Table &q, ScoreLds<S> *lds, const Operand &first, int qrow, int lane,
-                                   const int (&row0)[4], f32x4 (&acc)[4])
+__device__ inline float score_rows(const Table &t, const Table &q, ScoreLds<S> *lds, const Operand &first, int qrow, int lane,
+                                   const int (&row0)[4], float norm)
 {
     const int steps = (t.nb + 3) / 4, r = lane & 15, g = lane >> 4, at_lane = mx_staged_at(r, g);
-    bool ok[4] = {true, true, true, true};
     const bool whole = max(max(row0[0], row0[1]), max(row0[2], row0[3])) + 16 <= t.n;
-    const int last_row = g == 0 ? row0[0] : g == 1 ? row0[1] : g == 2 ? row0[2] : row0[3];
-    const uint8_t *lane_scales = t.scales + (size_t)min(last_row + r, t.n - 1) * t.sp;
-    const auto stage = [&](int s0) {
+    const int scale_row = (g == 0 ? row0[0] : g == 1 ? row0[1] : g == 2 ? row0[2] : row0[3]) + r;
+    const uint8_t *lane_scales = t.scales + (size_t)min(scale_row, t.n - 1) * t.sp;
+    const u32 lane_codes = __umul24(lane >> 2, t.nb) * 16;
+    f32x4 acc[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[i] = f32x4{norm, norm, norm, norm};
+    for (int s0 = 0; s0 < steps; s0 += S) {
 #pragma unroll
         for (int s = 0; s < S; ++s) {
             if (S > 1 && s0 + s >= steps) break;
-            const int block = mx_stage_block(lane, s0 + s, t.nb);
+            const u32 block = mx_stage_block(lane, s0 + s, t.nb) * 16;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int row = whole ? lane >> 2 : min(lane >> 2, t.n - 1 - row0[i]);
-                mx_stage(t.codes + (size_t)row0[i] * t.nb * 16 + (u32)(__umul24(row, t.nb) + block) * 16, &lds->codes[s * 4 + i][0], 1);
+                const u32 row = whole ? lane_codes : __umul24(min(lane >> 2, t.n - 1 - row0[i]), t.nb) * 16;
+                mx_stage(t.codes + (size_t)row0[i] * t.nb * 16 + (row + block), &lds->codes[s * 4 + i][0], 1);
             }
             mx_stage(lane_scales + 4 * (s0 + s), &lds->scales[s][0][0], 0);
         }
-    };
-    stage(0);
-    float top = 0.0f;
-    if (whole) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i] = *(const f32x4 *)(t.norms + row0[i] + 4 * g);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            top = __builtin_elementwise_maximum(__builtin_elementwise_maximum(top, __builtin_elementwise_maximum(acc[i][0], acc[i][1])),
-                                                __builtin_elementwise_maximum(acc[i][2], acc[i][3]));      // (a NaN stays)
-    }
-    if (!whole || __any(!mx_takes_part(top))) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int left = t.n - row0[i];
-            const float *norms = t.norms + row0[i];
-            const auto start = [&](int c) {
-                const float norm = norms[min(4 * g + c, left - 1)];
-                return 4 * g + c < left && mx_takes_part(norm) ? norm : __builtin_inff();
-            };
-            ok[i] = mx_takes_part(norms[min(r, left - 1)]);
-            acc[i] = f32x4{start(0), start(1), start(2), start(3)};
-        }
-    }
-    for (int s0 = 0; s0 < steps; s0 += S) {
-        if (s0 > 0) stage(s0);
         Operand y[S];
 #pragma unroll
         for (int s = 0; s < S; ++s) y[s] = S == 1 && s0 == 0 ? first : mx_query(q, qrow, 4 * (s0 + s) + g, true);
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        wait_loads<0>();
 #pragma unroll
         for (int s = 0; s < S; ++s) {
             if (S > 1 && s0 + s >= steps) break;
@@ -1154,13 +1140,20 @@ __device__ inline void score_tiles(const Table &t, const Table &q, ScoreLds<S> *
             for (int i = 0; i < 4; ++i) {
                 Operand x;
                 x.codes = *(const i32x4 *)&lds->codes[s * 4 + i][at_lane];
-                const int scale = ((const uint8_t *)&lds->scales[s][i][r])[block];
-                x.scale = ok[i] ? scale : 0;
+                x.scale = ((const uint8_t *)&lds->scales[s][i][r])[block];
                 acc[i] = mx_mma(x, y[s], acc[i]);
             }
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // (read before it is written again)
     }
+    float u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float lo = r & 1 ? acc[i][1] : acc[i][0], hi = r & 1 ? acc[i][3] : acc[i][2];
+        u[i] = r & 2 ? hi : lo;
+    }
+    const float lo = r & 4 ? u[1] : u[0], hi = r & 4 ? u[3] : u[2];
+    return r & 8 ? hi : lo;
 }
 
 // WAVES waves per query (one: many queries; several: few).  All of them choose the same supers and groups; the rows of
@@ -1200,31 +1193,24 @@ __global__ __launch_bounds__(64 * WAVES) void pick_kernel(Scan a, int k, long lo
         for (int i = lane; i < n_groups; i += 64) chosen[i] = mine[i];
         __builtin_amdgcn_wave_barrier();
         list.start(mine, kk);
-        // values of the groups' rows, four tiles of 16 at a time; every column of the instruction holds the query, and lane
-        // (g, r < 4) looks after row 4 g + r of a tile
+        // values of the groups' rows, four tiles of 16 at a time
         const Operand first = mx_query(q, a.first + qi, g, true);
         const float farthest = bound < kOrderInf ? mx_unorder(bound) : 3.402823466e+38f;
         const int per_group = group / 16, log_per_group = 31 - __clz(per_group), n_tiles = n_groups << log_per_group;
         for (int tile0 = wave * 4; tile0 < n_tiles; tile0 += WAVES * 4) {
-            int row0[4];
-            bool live[4];
-            f32x4 acc[4];
+            int row0[4], row_lane = 0;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int tile = min(tile0 + i, n_tiles - 1);
-                const int id = __builtin_amdgcn_readfirstlane((int)(u32)chosen[tile >> log_per_group]);
-                row0[i] = id * group + (tile & (per_group - 1)) * 16;
-                live[i] = tile0 + i < n_tiles && row0[i] < t.n;      // (the table can end inside a group)
-                row0[i] = live[i] ? row0[i] : 0;
+                const int at = __builtin_amdgcn_readfirstlane((int)(u32)chosen[tile >> log_per_group]) * group + (tile & (per_group - 1)) * 16;
+                if (r >> 2 == i) row_lane = at;
+                row0[i] = min(at, t.n - 1);            // (the table can end inside a group)
             }
-            score_tiles<S>(t, q, scores, first, a.first + qi, lane, row0, acc);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float u = r == 0 ? acc[i][0] : r == 1 ? acc[i][1] : r == 2 ? acc[i][2] : acc[i][3];
-                const int id = row0[i] + 4 * g + r;
-                const bool take = r < 4 && u <= farthest && id != self && live[i];
-                if (__any(take)) list.push(((u64)mx_order(u) << 32) | (u32)id, take, lane);
-            }
+            const int id = row_lane + 4 * g + (r & 3);
+            const float norm = t.norms[min(id, t.n - 1)];
+            const float u = score_rows<S>(t, q, scores, first, a.first + qi, lane, row0, norm);
+            const bool take = u <= farthest && id != self && id < t.n && tile0 + (r >> 2) < n_tiles && mx_takes_part(norm);
+            if (__any(take)) list.push(((u64)mx_order(u) << 32) | (u32)id, take, lane);
             if (list.count > kListRoom - 64) list.cut(lane);
         }
     }
