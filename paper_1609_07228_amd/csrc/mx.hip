@@ -937,28 +937,54 @@ __global__ __launch_bounds__(256, 2) void scan_narrow_kernel(Scan a)
     }
 }
 
-// A word that separates the `want` smallest of a wave's 64 * R words (want <= 64 * R) from the others, bit by bit: exactly
-// `want` of them do not exceed it (sharp), or it is the want-th smallest, which others equal; `less` are smaller then.
+// One word from all of a wave's, by an operation that does not mind order or repetition
+template <class Of> __device__ inline u32 wave_all(u32 x, Of of)
+{
+    x = of(x, mx_from<kSwap1>(x));
+    x = of(x, mx_from<kSwap2>(x));
+    x = of(x, mx_from<kDown4>(x));
+    x = of(x, mx_from<kDown8>(x));
+    const u32 a = __builtin_amdgcn_readlane(x, 0), b = __builtin_amdgcn_readlane(x, 16);
+    const u32 c = __builtin_amdgcn_readlane(x, 32), d = __builtin_amdgcn_readlane(x, 48);
+    return of(of(a, b), of(c, d));
+}
+
+// A word that separates the `want` smallest of a wave's 64 * R words from the others, bit by bit: exactly `want` of them do not
+// exceed it (sharp), or it is the want-th smallest, which others equal; `less` are smaller then.  A word of all ones stands for
+// nothing, and `want` at least are something.  The search counts from the smallest word on and leaves out the leading and the last
+// bits that no word has there: values next to one another share the leading ones, products of codes end in zeros.
 template <int R>
 __device__ inline u32 wave_nth(const u32 (&v)[R], int want, int &less, bool &sharp)
 {
+    u32 low = v[0];
+#pragma unroll
+    for (int i = 1; i < R; ++i) low = min(low, v[i]);
+    low = wave_all(low, [](u32 a, u32 b) { return min(a, b); });
+    u32 above[R], bits = 0;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        above[i] = v[i] - low;
+        bits |= v[i] == ~0u ? 0 : above[i];
+    }
+    bits = wave_all(bits, [](u32 a, u32 b) { return a | b; });
     u32 t = 0;
     less = 0;
     sharp = false;
-    for (u32 bit = 0x80000000u; bit != 0; bit >>= 1) {
+    const u32 last = bits & (0 - bits);
+    for (u32 bit = bits ? 0x80000000u >> __clz(bits) : 0; bit >= last && bit != 0; bit >>= 1) {
         int n = 0;
 #pragma unroll
-        for (int i = 0; i < R; ++i) n += __popcll(__ballot(v[i] < t + bit));
+        for (int i = 0; i < R; ++i) n += __popcll(__ballot(above[i] < t + bit));
         if (n == want) {
             sharp = true;
-            return t + bit - 1;
+            return low + min(t + bit - 1, ~0u - 1 - low);
         }
         if (n < want) {
             t += bit;
             less = n;
         }
     }
-    return t;
+    return low + t;
 }
 
 // The smallest keys (word, index) that a wave has met, in LDS.  limit: a key that `want` keys of the list do not
