@@ -137,7 +137,9 @@ __global__ __launch_bounds__(256) void quantise_kernel(const T *X, long long n, 
 
 // ---- rows by id ------------------------------------------------------------------------------------------
 // A lane per 16 bytes of an output row (4 or 8 coordinates: neighbouring lanes' stores touch), `group` lanes (a power of two)
-// per row and kRows rows per lane, so that as many chains of id, codes, store run side by side.  Bound: HBM writes.
+// per row and kRows rows per lane, so that as many chains of id, codes, store run side by side.  Bound: HBM writes (2 * 10^6 rows of
+// 128 by id to bf16, 512 MB: 92 us, 5.6 TB/s; 10^6 rows to float32: 91 us, 6.4 TB/s with the table).  Codes have two significant
+// bits, so value * scale is exact; the factor's product is rounded to float32 and then once to the output's type.
 constexpr int kRows = 4;
 template <class T, bool PAST_CACHE>
 __global__ __launch_bounds__(256) void rows_kernel(Table t, int d, const int *ids, long long m, int group, float factor, T *out)
@@ -243,8 +245,11 @@ template <int N> __device__ inline void wait_loads() { asm volatile("s_waitcnt v
 // coordinates of both, whole lines of 128 bytes (half lines cost the loads as much each), and the scales of 512 coordinates
 // with every other one; while one is computed the next is on its way into LDS.  A load of codes brings 8 rows; the blocks of row
 // r lie in the order b ^ (r / 2) % 8, so that blocks b of 16 rows, which are read together, are in different ones of the 64 banks.
-// A wave reads (FA + FB) KiB from LDS for FA * FB instructions of 32 cycles; with four waves of 4 x 4 LDS is busy for 0.6 of
-// them, with eight of 4 x 2 for 0.9.
+// Bound: clocks under load, then what a stage waits for.  8192^3 takes 0.28 ms, 3.9 PFLOP/s, at 1.7 GHz with the matrix units busy for
+// 0.54 and LDS for 0.33 of the time; all loads from the same eight rows (less to move and fewer bits that change) 0.24.
+// Tiles of 128 x 128, two workgroups a CU, 0.36: they load twice as much.  Long outputs of short sums wait for their stores too:
+// 4096 x 65536 x 960 to bf16 0.26 ms, of which 0.1 go with the stores; workgroups that stay and ask for the next tile before they
+// store this one were no faster, and 0.27 with stores past the caches.
 template <int FA, int FB, int WA, int WB>
 struct Tiling {
     static constexpr int waves = WA * WB, side_a = 32 * FA * WA, side_b = 32 * FB * WB, sides = side_a + side_b;
@@ -436,7 +441,7 @@ __global__ __launch_bounds__(64 * WA * WB, FA * FB > 8 ? 1 : 2) void product_til
     }
 }
 
-// Few rows of a (16 * M at most): bound by reading b once.  A wave takes 64 rows of b and its share of the steps, S of them in
+// Few rows of a (16 * M at most): bound by reading b once (one row against 10^6 x 128: 12 us, 5.9 TB/s with the output).  A wave takes 64 rows of b and its share of the steps, S of them in
 // flight; the WAVES waves of a workgroup take the same rows, and their sums meet in LDS, in the waves' order.
 template <int S>
 struct FewLds {
@@ -778,7 +783,9 @@ __device__ inline f32x4 mx_start(const Lds *l, int tile, int g, int left)
 }
 
 // Many queries: a workgroup of 8 waves holds 8 * QF * 16 queries in registers and passes the rows of its supers
-// through LDS, a stage of about kStage operands at a time, loaded while the stage before is computed.
+// through LDS, a stage of about kStage operands at a time, loaded while the stage before is computed.  Bound: clocks under load
+// (10 000 queries of 10^6 x 128: 0.56 ms, 4.6 PFLOP/s, the matrix units busy for 0.57 of the time at 1.9 GHz and other vector
+// instructions, two minima per matrix instruction most of all, for as much; 1000 of 10^6 x 960: 0.43 ms, 4.5 PFLOP/s).
 constexpr int kStage = 32;
 
 template <int KS, int QF>
@@ -872,7 +879,7 @@ __global__ __launch_bounds__(512, KS == 1 ? 4 : 2) void scan_wide_kernel(Scan a)
 }
 
 // Few queries: all four waves of a workgroup hold the same QF * 16 of them and take a block of a super each, up to 16
-// operands of it in flight.  Bound by HBM: the rows are read once.
+// operands of it in flight.  Bound by HBM: the rows are read once (one query of 10^6 x 128, 72 MB: 14.5 us, 5.0 TB/s).
 template <int KS, int QF>
 __global__ __launch_bounds__(256, 2) void scan_narrow_kernel(Scan a)
 {
@@ -1183,6 +1190,8 @@ __device__ inline float score_rows(const Table &t, const Table &q, ScoreLds<S> *
     return r & 8 ? hi : lo;
 }
 
+// Bound: instructions and their latency (20 003 queries of as many rows of 50: 86 us, 1100 vector and 1600 scalar instructions per
+// query; 10 000 of 10^6 x 128: 100 us; one: 13.5 us, a chain of some thirty dependent steps).
 // WAVES waves per query (one: many queries; several: few).  All of them choose the same supers and groups; the rows of
 // the groups are shared out, and the waves' lists meet in the first one's.
 template <int WAVES, int S>
