@@ -331,11 +331,16 @@ def _mx_dtype(dtype: torch.dtype) -> int:
 
 def _mx_table(t: MxTable) -> int:
     """Checks a table's tensors against one another; returns its row count."""
-    n, nb = t.codes.shape[0], (t.d + 31) // 32
-    _dev(t.codes, torch.uint8), _dev(t.scales, torch.uint8), _dev(t.norms, torch.float32)
-    if t.codes.shape != (n, 16 * nb) or t.scales.shape != (n, (nb + 3) // 4 * 4) or t.norms.shape != (n,):
+    codes, scales, norms, d = t
+    n, nb = codes.shape[0], (d + 31) // 32
+    # (in few calls: a small table's kernel takes less time than its checks)
+    if codes.dtype is not torch.uint8 or scales.dtype is not torch.uint8 or norms.dtype is not torch.float32:
+        raise ValueError("expected codes and scales in uint8 and norms in float32")
+    if codes.shape != (n, 16 * nb) or scales.shape != (n, (nb + 3) // 4 * 4) or norms.shape != (n,):
         raise ValueError("codes, scales and norms do not make a table of d coordinates")
-    if t.codes.device != t.scales.device or t.codes.device != t.norms.device:
+    if not (codes.is_cuda and codes.is_contiguous() and scales.is_contiguous() and norms.is_contiguous()):
+        raise ValueError("expected contiguous device tensors")
+    if not codes.get_device() == scales.get_device() == norms.get_device():
         raise ValueError("a table's tensors are on different devices")
     return n
 
@@ -374,11 +379,11 @@ def efanna_mx_rows(table: MxTable, ids: torch.Tensor | None = None, factor: floa
         if ids.device != table.codes.device:
             raise ValueError("ids and table are on different devices")
     m = n if ids is None else ids.numel()
-    out = torch.empty((m, table.d), dtype=dtype, device=table.codes.device)
+    out = torch.empty((n, table.d) if ids is None else (*ids.shape, table.d), dtype=dtype, device=table.codes.device)
     _check(lib().efanna_mx_rows(table.codes.data_ptr(), table.scales.data_ptr(), n, table.d,
                                 None if ids is None else ids.data_ptr(), m, float(factor), code, out.data_ptr(), _stream()),
            "efanna_mx_rows")
-    return out if ids is None else out.view(*ids.shape, table.d)
+    return out
 
 
 def efanna_mx_product(a: MxTable, b: MxTable, dtype: torch.dtype = torch.float32,
