@@ -1357,7 +1357,9 @@ template <int KS>
 int launch_scan(const Scan &a, hipStream_t st)
 {
     if (a.nq <= 16) return launch_narrow<KS, 1>(a, st);
-    if (a.nq <= 64) return launch_narrow<KS, 4>(a, st);
+    // (64 queries' operands of longer rows leave too few registers: 32 of 10^6 x 832 137 us, otherwise 144; of 10^6 x 960 166 and 152)
+    if constexpr (KS <= 7)
+        if (a.nq <= 64) return launch_narrow<KS, 4>(a, st);
     if (a.nq <= 128) return launch_wide<KS, 1>(a, st);
     if (a.nq <= 256) return launch_wide<KS, 2>(a, st);
     if (a.nq <= 512 || KS > 4) return launch_wide<KS, 4>(a, st);

@@ -40,3 +40,20 @@ def test_few_different_distances(ef, n, k, nq):
         want = (dist * 2 ** 20 + row).topk(k, largest=False).indices        # (distance, id): 2^20 is more than the rows
         assert torch.equal(ids[i].to(torch.int64), want)
         assert torch.equal(dists[i].to(torch.float64), dist[want])
+
+
+@pytest.mark.parametrize("d", [640, 768, 800, 960, 1024])
+@pytest.mark.parametrize("nq", [16, 17, 40, 64, 65])
+def test_long_rows_and_tens_of_queries(ef, d, nq):
+    """Whole numbers, so that sums are exact; the last group is not full."""
+    gen = torch.Generator(device="cuda").manual_seed(d + nq)
+    n, k = 2777, 12
+    x = torch.randint(-2, 3, (n, d), generator=gen, device="cuda").to(torch.float32)
+    y = torch.randint(-2, 3, (nq, d), generator=gen, device="cuda").to(torch.float32)
+    x[:, ::32], y[:, ::32] = 4.0, 4.0                    # every block's scale is 1
+    ids, dists = ef.efanna_mx_nearest(ef.efanna_mx_quantise(x), ef.efanna_mx_quantise(y), k)
+    X, Q = x.to(torch.float64), y.to(torch.float64)
+    dist = Q.square().sum(dim=1, keepdim=True) + X.square().sum(dim=1) - 2 * (Q @ X.T)
+    want = (dist * 4096 + torch.arange(n, device="cuda")).topk(k, dim=1, largest=False).indices
+    assert torch.equal(ids.to(torch.int64), want)
+    assert torch.equal(dists.to(torch.float64), dist.gather(1, want))
