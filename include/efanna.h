@@ -65,6 +65,7 @@ typedef enum {
 #define EFANNA_MAX_LEAF 64      /* leaf population S                                   */
 #define EFANNA_MAX_TREES 64
 #define EFANNA_MX_MAX_D 65536   /* coordinates of a row of an MXFP4 table              */
+#define EFANNA_MX_MAX_NORM 8.507059173023462e37f   /* 2^126: squared lengths that have neighbours are below */
 /* size of the fixed device array behind efanna_nndescent_noalloc (64 MiB per GPU in use) */
 #define EFANNA_NOALLOC_SCRATCH_BYTES (64u << 20)
 
@@ -341,8 +342,9 @@ int efanna_mx_product(const uint8_t *a_codes, const uint8_t *a_scales, int64_t m
  * (s descending, id ascending), s = q.x - |x|^2 / 2 in float32 with |x|^2 taken from norms.
  * That is the order (squared distance, id) of the rows as held, up to the rounding of s; s is exact
  * wherever the terms of a sum span no more than 24 bits.
- * norms, q_norms [device] as efanna_mx_quantise writes them (norms 16-byte aligned).  A row whose
- *        norm is not finite is nobody's neighbour, a query whose norm is not finite has none.
+ * norms, q_norms [device] as efanna_mx_quantise writes them (norms 16-byte aligned).  Only norms below
+ *        EFANNA_MX_MAX_NORM take part, so that no sum and no distance leaves the float32 range: a row
+ *        of a larger norm, or of none (NaN), is nobody's neighbour, and such a query has none.
  * first_self >= 0: query i is row first_self + i of the table and not its own neighbour; -1: none is.
  * ids, dists [device] out, nq * k int32 / float32: ids and max(0, |q|^2 - 2 s), nearest first; -1 and
  *        +inf where there are fewer than k.

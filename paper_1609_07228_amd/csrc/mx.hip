@@ -579,8 +579,7 @@ int launch_product(const Table &a, const Table &b, T *out, int64_t ldo, hipStrea
 // Four groups are passed over together ("block"): tile t of `tiles` holds as instruction row r the block's row
 // (r / 4) * 4 tiles + 4 t + r % 4, so that the four values of a lane belong to one group in every tile and its
 // running minimum needs no other lane.  A group is 4 tiles rows, a super four blocks.
-constexpr float kNormLimit = 8.507059173023462e37f;      // 2^126
-__device__ inline bool mx_takes_part(float norm) { return norm < kNormLimit; }
+__device__ inline bool mx_takes_part(float norm) { return norm < EFANNA_MX_MAX_NORM; }
 __device__ inline float mx_min(float a, float b) { return __builtin_elementwise_minimum(a, b); }
 
 // smaller value <-> smaller word; -0 and 0 the same

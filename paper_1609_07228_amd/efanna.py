@@ -320,6 +320,8 @@ class MxTable(NamedTuple):
     d: int
 
 
+MX_MAX_NORM = 2.0 ** 126      # EFANNA_MX_MAX_NORM: rows and queries of this squared length or more have no neighbours
+
 _MX_DTYPE = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 
@@ -404,7 +406,8 @@ def efanna_mx_nearest(table: MxTable, queries: MxTable, k: int, first_self: int 
                       workspace: torch.Tensor | None = None):
     """The k nearest rows of `table` to every row of `queries`, all rows compared: (ids [nq, k] int32, dists [nq, k]
     float32, squared distances of the rows as held), nearest first, equal ones by id; -1 and +inf where there are
-    fewer.  first_self >= 0: query i is row first_self + i of the table and not its own neighbour."""
+    fewer.  first_self >= 0: query i is row first_self + i of the table and not its own neighbour.  Rows and queries whose
+    norm is not below MX_MAX_NORM (or is NaN) are nobody's neighbours and have none."""
     n, nq = _mx_table(table), _mx_table(queries)
     if table.d != queries.d or table.codes.device != queries.codes.device:
         raise ValueError("the tables differ in their dimension or device")

@@ -1,0 +1,64 @@
+"""MXFP4 tables at the limits that the header states: squared lengths next to the largest that have neighbours."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ef():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a GPU: there is no CPU fallback")
+    from paper_1609_07228_amd import efanna
+    return efanna
+
+
+# Squares of one block's values in units of 2^120 (scale 2^60, largest value 6): 64 of them are 2^126, 256 are 2^128.
+JUST_BELOW = [6, 4, 3, 1.5, 0.5, 0.5]                 # 63.75: the nearest squared length below
+JUST_AT = [6, 4, 3, 1.5, 0.5, 0.5, 0.5]               # 64
+NEAR_THE_END = [6] * 7 + [1.5, 0.5, 0.5, 0.5]         # 255: finite in float32
+BEYOND = [6] * 7 + [2]                                # 256: infinite
+
+
+def rows(kinds, signs=None):
+    x = np.zeros((len(kinds), 32), np.float32)
+    for i, kind in enumerate(kinds):
+        x[i, :len(kind)] = np.array(kind, np.float32) * np.float32(2.0) ** 60
+        if signs is not None:
+            x[i] *= signs[i]
+    return x
+
+
+@pytest.mark.parametrize("nq", [1, 40, 200])
+@pytest.mark.parametrize("d", [32, 1100])
+def test_rows_and_queries_on_both_sides_of_the_largest_norm(ef, nq, d):
+    """Everything is a whole number of 2^118, so distances are exact."""
+    kinds = [JUST_BELOW, JUST_AT, [0], NEAR_THE_END, [6], BEYOND, [0.5], JUST_BELOW, [-6], JUST_AT]
+    x = np.zeros((len(kinds) * 30, d), np.float32)
+    x[:, :32] = np.tile(rows(kinds), (30, 1))
+    x[::7, :32] *= -1
+    if d > 32:
+        x[5::11, 1056:1088] = x[5::11, :32]           # the same in a block of its own, at the end of the row
+        x[5::11, :32] = 0
+    y = np.concatenate([x[:13], x[-7:]])
+    y = np.tile(y, (nq // len(y) + 1, 1))[:nq]
+    t, q = ef.efanna_mx_quantise(torch.from_numpy(x).cuda()), ef.efanna_mx_quantise(torch.from_numpy(y).cuda())
+    X, Q = x.astype(np.float64), y.astype(np.float64)
+    assert np.array_equal(ef.efanna_mx_rows(t).cpu().numpy(), x)          # the format holds them
+    xx, qq = (X * X).sum(axis=1), (Q * Q).sum(axis=1)
+    with np.errstate(over="ignore"):
+        assert np.array_equal(t.norms.cpu().numpy(), xx.astype(np.float32))
+    limit = ef.MX_MAX_NORM
+    assert {0.0, limit * 63.75 / 64, limit, limit * 255 / 64} <= set(xx)
+    ids, dists = (o.cpu().numpy() for o in ef.efanna_mx_nearest(t, q, 128))
+    near = np.nonzero(xx < limit)[0]
+    assert len(near) > 128 and (xx >= limit).any()
+    for i in range(nq):
+        if not qq[i] < limit:
+            assert (ids[i] == -1).all() and np.isinf(dists[i]).all()
+            continue
+        dist = qq[i] + xx[near] - 2 * (X[near] @ Q[i])
+        by = np.argsort(dist, kind="stable")[:128]
+        assert np.array_equal(ids[i], near[by])
+        assert np.array_equal(dists[i].astype(np.float64), dist[by])
