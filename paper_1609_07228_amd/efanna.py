@@ -93,9 +93,16 @@ def _check(status: int, where: str):
         raise EfannaError(status, where)
 
 
-def _stream() -> int:
-    # torch.cuda.current_stream().cuda_stream without the object around it (0.3 us instead of 2.8)
-    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+def _call(name: str, on: torch.Tensor, *args):
+    """Calls an entry point with `args` and, after them, the current stream of the GPU that holds `on`, which is the current
+    GPU meanwhile (kernels and events go to that one)."""
+    gpu = on.get_device()
+    if gpu == torch._C._cuda_getDevice():
+        # torch.cuda.current_stream().cuda_stream without the object around it (0.3 us instead of 2.8)
+        _check(getattr(lib(), name)(*args, torch._C._cuda_getCurrentRawStream(gpu)), name)
+        return
+    with torch.cuda.device(gpu):
+        _check(getattr(lib(), name)(*args, torch._C._cuda_getCurrentRawStream(gpu)), name)
 
 
 def _dev(t: torch.Tensor, dtype) -> torch.Tensor:
@@ -149,12 +156,11 @@ def efanna_build_trees(X: torch.Tensor, n_trees: int, leaf_size: int, seed: int,
     ws = _workspace(need, X.device) if workspace is None else workspace
     tail = (perm.data_ptr(), leaf_off.data_ptr(), max_leaves, n_leaves.ctypes.data_as(C.c_void_p),
             nodes.data_ptr() if with_nodes else None, leaf_up.data_ptr() if with_nodes else None,
-            C.byref(depth), ws.data_ptr(), ws.numel(), _stream())
+            C.byref(depth), ws.data_ptr(), ws.numel())
     if _rule is None:
-        _check(lib().efanna_build_trees(X.data_ptr(), n, d, n_trees, leaf_size, seed, *tail), "efanna_build_trees")
+        _call("efanna_build_trees", X, X.data_ptr(), n, d, n_trees, leaf_size, seed, *tail)
     else:
-        _check(lib().efanna_build_trees_rule(X.data_ptr(), n, d, n_trees, leaf_size, seed, _rule, *tail),
-               "efanna_build_trees_rule")
+        _call("efanna_build_trees_rule", X, X.data_ptr(), n, d, n_trees, leaf_size, seed, _rule, *tail)
     if with_nodes:
         return perm, leaf_off, n_leaves, nodes, leaf_up, int(depth.value)
     return perm, leaf_off, n_leaves
@@ -186,12 +192,12 @@ def efanna_init_graph(X: torch.Tensor, perm: torch.Tensor, leaf_off: torch.Tenso
     levels = 0 if nodes is None else int(tree_depth) - int(conquer_depth) + 1
     need = lib().efanna_init_workspace_bytes(n, levels)
     ws = _workspace(need, X.device) if workspace is None else workspace
-    _check(lib().efanna_init_graph(X.data_ptr(), n, d, perm.data_ptr(), leaf_off.data_ptr(),
-                                   leaf_off.shape[1] - 1, n_leaves.ctypes.data_as(C.c_void_p),
-                                   nodes.data_ptr() if nodes is not None else None,
-                                   leaf_up.data_ptr() if nodes is not None else None,
-                                   int(tree_depth), int(conquer_depth), T, leaf_size, k, graph.data_ptr(),
-                                   ws.data_ptr(), ws.numel(), _stream()), "efanna_init_graph")
+    _call("efanna_init_graph", X, X.data_ptr(), n, d, perm.data_ptr(), leaf_off.data_ptr(),
+          leaf_off.shape[1] - 1, n_leaves.ctypes.data_as(C.c_void_p),
+          nodes.data_ptr() if nodes is not None else None,
+          leaf_up.data_ptr() if nodes is not None else None,
+          int(tree_depth), int(conquer_depth), T, leaf_size, k, graph.data_ptr(),
+          ws.data_ptr(), ws.numel())
     return graph
 
 
@@ -217,10 +223,10 @@ def efanna_nndescent(X: torch.Tensor, graph: torch.Tensor, iters: int, sample_L:
     need = lib().efanna_nndescent_workspace_bytes(n, k, sample_L)
     ws = _workspace(need, X.device) if workspace is None else workspace
     done = C.c_int32(0)
-    _check(lib().efanna_nndescent(X.data_ptr(), n, d, k, graph.data_ptr(), iters, sample_L, seed,
-                                  first_iter, float(delta), 1 if cross_old else 0, C.byref(done), stats.data_ptr(),
-                                  None if phase_ms is None else phase_ms.ctypes.data_as(C.c_void_p),
-                                  ws.data_ptr(), ws.numel(), _stream()), "efanna_nndescent")
+    _call("efanna_nndescent", X, X.data_ptr(), n, d, k, graph.data_ptr(), iters, sample_L, seed,
+          first_iter, float(delta), 1 if cross_old else 0, C.byref(done), stats.data_ptr(),
+          None if phase_ms is None else phase_ms.ctypes.data_as(C.c_void_p),
+          ws.data_ptr(), ws.numel())
     if delta > 0.0:
         return stats[:done.value], int(done.value)
     return stats[:iters]
@@ -236,9 +242,8 @@ def efanna_nndescent_noalloc(X: torch.Tensor, graph: torch.Tensor, iters: int, s
     stats = _dev(stats, torch.int64)
     if stats.numel() < 4 * max(iters, 1):
         raise ValueError("stats holds fewer than 4 * iters values")
-    _check(lib().efanna_nndescent_noalloc(X.data_ptr(), n, d, graph.shape[1], graph.data_ptr(), iters,
-                                          sample_L, seed, first_iter, stats.data_ptr(), _stream()),
-           "efanna_nndescent_noalloc")
+    _call("efanna_nndescent_noalloc", X, X.data_ptr(), n, d, graph.shape[1], graph.data_ptr(), iters,
+          sample_L, seed, first_iter, stats.data_ptr())
     return stats
 
 
@@ -249,9 +254,8 @@ def efanna_get_graph(graph: torch.Tensor, with_flags: bool = False):
     ids = torch.empty((n, k), dtype=torch.int32, device=graph.device)
     dists = torch.empty((n, k), dtype=torch.float32, device=graph.device)
     flags = torch.empty((n, k), dtype=torch.uint8, device=graph.device) if with_flags else None
-    _check(lib().efanna_get_graph(graph.data_ptr(), n, k, ids.data_ptr(), dists.data_ptr(),
-                                  flags.data_ptr() if with_flags else None, _stream()),
-           "efanna_get_graph")
+    _call("efanna_get_graph", graph, graph.data_ptr(), n, k, ids.data_ptr(), dists.data_ptr(),
+          flags.data_ptr() if with_flags else None)
     return (ids, dists, flags) if with_flags else (ids, dists)
 
 
@@ -263,9 +267,8 @@ def efanna_set_graph(ids: torch.Tensor, dists: torch.Tensor, flags: torch.Tensor
     if flags is not None:
         flags = _dev(flags, torch.uint8)
     graph = torch.empty((n, k), dtype=torch.int64, device=ids.device)
-    _check(lib().efanna_set_graph(graph.data_ptr(), n, k, ids.data_ptr(), dists.data_ptr(),
-                                  flags.data_ptr() if flags is not None else None, _stream()),
-           "efanna_set_graph")
+    _call("efanna_set_graph", graph, graph.data_ptr(), n, k, ids.data_ptr(), dists.data_ptr(),
+          flags.data_ptr() if flags is not None else None)
     return graph
 
 
@@ -274,9 +277,8 @@ def efanna_pair_distances(X: torch.Tensor, a_ids: torch.Tensor, b_ids: torch.Ten
     a_ids = _dev(a_ids, torch.int32)
     b_ids = _dev(b_ids, torch.int32)
     out = torch.empty(a_ids.shape[0], dtype=torch.float32, device=X.device)
-    _check(lib().efanna_pair_distances(X.data_ptr(), X.shape[0], X.shape[1], a_ids.data_ptr(),
-                                       b_ids.data_ptr(), a_ids.shape[0], out.data_ptr(), _stream()),
-           "efanna_pair_distances")
+    _call("efanna_pair_distances", X, X.data_ptr(), X.shape[0], X.shape[1], a_ids.data_ptr(),
+          b_ids.data_ptr(), a_ids.shape[0], out.data_ptr())
     return out
 
 
@@ -303,11 +305,11 @@ def efanna_search(X: torch.Tensor, perm: torch.Tensor, leaf_off: torch.Tensor, n
     checked = torch.empty((nq,), dtype=torch.int32, device=X.device)
     need = lib().efanna_search_workspace_bytes(nq, d, T, leaf_size, tree_depth, g.shape[1], pool, iters)
     ws = _workspace(need, X.device) if workspace is None else workspace
-    _check(lib().efanna_search(X.data_ptr(), n, d, perm.data_ptr(), leaf_off.data_ptr(),
-                               leaf_off.shape[1] - 1, n_leaves.ctypes.data_as(C.c_void_p),
-                               nodes.data_ptr(), int(tree_depth), T, leaf_size, g.data_ptr(), g.shape[1],
-                               Q.data_ptr(), nq, k, pool, expand, iters, ids.data_ptr(), dists.data_ptr(),
-                               checked.data_ptr(), ws.data_ptr(), ws.numel(), _stream()), "efanna_search")
+    _call("efanna_search", X, X.data_ptr(), n, d, perm.data_ptr(), leaf_off.data_ptr(),
+          leaf_off.shape[1] - 1, n_leaves.ctypes.data_as(C.c_void_p),
+          nodes.data_ptr(), int(tree_depth), T, leaf_size, g.data_ptr(), g.shape[1],
+          Q.data_ptr(), nq, k, pool, expand, iters, ids.data_ptr(), dists.data_ptr(),
+          checked.data_ptr(), ws.data_ptr(), ws.numel())
     return ids, dists, checked
 
 
@@ -366,8 +368,7 @@ def efanna_mx_quantise(X: torch.Tensor) -> MxTable:
     codes = torch.empty((n, 16 * nb), dtype=torch.uint8, device=X.device)
     scales = torch.empty((n, (nb + 3) // 4 * 4), dtype=torch.uint8, device=X.device)
     norms = torch.empty((n,), dtype=torch.float32, device=X.device)
-    _check(lib().efanna_mx_quantise(X.data_ptr(), code, n, d, ldx, codes.data_ptr(), scales.data_ptr(), norms.data_ptr(),
-                                    _stream()), "efanna_mx_quantise")
+    _call("efanna_mx_quantise", X, X.data_ptr(), code, n, d, ldx, codes.data_ptr(), scales.data_ptr(), norms.data_ptr())
     return MxTable(codes, scales, norms, d)
 
 
@@ -382,9 +383,8 @@ def efanna_mx_rows(table: MxTable, ids: torch.Tensor | None = None, factor: floa
             raise ValueError("ids and table are on different devices")
     m = n if ids is None else ids.numel()
     out = torch.empty((n, table.d) if ids is None else (*ids.shape, table.d), dtype=dtype, device=table.codes.device)
-    _check(lib().efanna_mx_rows(table.codes.data_ptr(), table.scales.data_ptr(), n, table.d,
-                                None if ids is None else ids.data_ptr(), m, float(factor), code, out.data_ptr(), _stream()),
-           "efanna_mx_rows")
+    _call("efanna_mx_rows", table.codes, table.codes.data_ptr(), table.scales.data_ptr(), n, table.d,
+          None if ids is None else ids.data_ptr(), m, float(factor), code, out.data_ptr())
     return out
 
 
@@ -397,8 +397,8 @@ def efanna_mx_product(a: MxTable, b: MxTable, dtype: torch.dtype = torch.float32
         raise ValueError("the tables differ in their dimension or device")
     out = _mx_out(out, (m, n), dtype, a.codes.device)
     ldo = out.stride(0) if m > 1 else max(n, 1)
-    _check(lib().efanna_mx_product(a.codes.data_ptr(), a.scales.data_ptr(), m, b.codes.data_ptr(), b.scales.data_ptr(), n,
-                                   a.d, code, out.data_ptr(), ldo, _stream()), "efanna_mx_product")
+    _call("efanna_mx_product", a.codes, a.codes.data_ptr(), a.scales.data_ptr(), m, b.codes.data_ptr(), b.scales.data_ptr(),
+          n, a.d, code, out.data_ptr(), ldo)
     return out
 
 
@@ -415,8 +415,7 @@ def efanna_mx_nearest(table: MxTable, queries: MxTable, k: int, first_self: int 
     ids = torch.empty((nq, max(k, 0)), dtype=torch.int32, device=device)
     dists = torch.empty((nq, max(k, 0)), dtype=torch.float32, device=device)
     ws = _workspace(lib().efanna_mx_nearest_workspace_bytes(n, table.d, nq, k), device) if workspace is None else workspace
-    _check(lib().efanna_mx_nearest(table.codes.data_ptr(), table.scales.data_ptr(), table.norms.data_ptr(), n, table.d,
-                                   queries.codes.data_ptr(), queries.scales.data_ptr(), queries.norms.data_ptr(), nq, k,
-                                   int(first_self), ids.data_ptr(), dists.data_ptr(), ws.data_ptr(), ws.numel(), _stream()),
-           "efanna_mx_nearest")
+    _call("efanna_mx_nearest", table.codes, table.codes.data_ptr(), table.scales.data_ptr(), table.norms.data_ptr(), n,
+          table.d, queries.codes.data_ptr(), queries.scales.data_ptr(), queries.norms.data_ptr(), nq, k,
+          int(first_self), ids.data_ptr(), dists.data_ptr(), ws.data_ptr(), ws.numel())
     return ids, dists
