@@ -26,6 +26,9 @@ constexpr int kFp4 = 4;                    // the operand format's number in the
 // for whoever reads them next.
 constexpr int64_t kStreamBytes = (int64_t)32 << 20;
 constexpr size_t kMaxWorkspace = (size_t)1 << 30;
+// A launch takes fewer than 2^32 threads.  Rows that a kernel takes one by one go in slices of so many workgroups of 256.
+constexpr int64_t kSliceBlocks = (int64_t)1 << 23;
+inline bool launch_fits(int64_t blocks, int64_t threads) { return blocks <= 4294967295LL / threads; }
 
 // (64 KiB and less need no leave, and asking for it takes a microsecond)
 inline hipError_t allow_lds(const void *kernel, int bytes)
@@ -533,7 +536,7 @@ int launch_tiles(const Table &a, const Table &b, T *out, int64_t ldo, hipStream_
     const int lds = stages > turn ? stages : turn;
     EF_HIP_CHECK(allow_lds((const void *)product_tile_kernel<T, FA, FB, WA, WB>, lds));
     const int64_t ta = (a.n + Tile::side_a - 1) / Tile::side_a, tb = (b.n + Tile::side_b - 1) / Tile::side_b;
-    if (ta * tb > 2147483647LL) return EFANNA_EUNSUPPORTED;
+    if (ta * tb > 2147483647LL || !launch_fits(ta * tb, 64 * Tile::waves)) return EFANNA_EUNSUPPORTED;
     product_tile_kernel<T, FA, FB, WA, WB><<<(unsigned)(ta * tb), 64 * Tile::waves, lds, st>>>(a, b, out, ldo, (int)ta, (int)tb);
     return EFANNA_OK;
 }
@@ -541,8 +544,10 @@ template <class T, int M, int S, int WAVES>
 int launch_few(const Table &a, const Table &b, T *out, int64_t ldo, hipStream_t st)
 {
     const int stage = WAVES * (int)sizeof(FewLds<S>), join = (WAVES - 1) * M * 4 * 64 * 16, lds = stage > join ? stage : join;
+    const int64_t blocks = ((int64_t)b.n + 63) / 64;
+    if (!launch_fits(blocks, 64 * WAVES)) return EFANNA_EUNSUPPORTED;
     EF_HIP_CHECK(allow_lds((const void *)product_few_kernel<T, M, S, WAVES>, lds));
-    product_few_kernel<T, M, S, WAVES><<<(unsigned)((b.n + 63) / 64), 64 * WAVES, lds, st>>>(a, b, out, ldo);
+    product_few_kernel<T, M, S, WAVES><<<(unsigned)blocks, 64 * WAVES, lds, st>>>(a, b, out, ldo);
     return EFANNA_OK;
 }
 template <class T, int M>
@@ -1289,6 +1294,7 @@ inline NearestShape nearest_shape(int64_t n, int d, int64_t nq, int k)
     const size_t per16 = (size_t)s.supers * 17 * 16 * sizeof(float);     // 16 queries: groups and supers
     size_t sixteens = per16 ? kMaxWorkspace / per16 : (size_t)nq;
     if (sixteens < 16) sixteens = 16;
+    if (sixteens > (size_t)1 << 20) sixteens = (size_t)1 << 20;      // (no rows: what one launch of the choice takes)
     const size_t all = (size_t)(nq + 15) / 16;
     if (sixteens >= all) sixteens = all;
     else {                         // passes of equal size
@@ -1340,7 +1346,7 @@ int launch_wide(Scan a, hipStream_t st)
     }
     const int64_t slices = (a.supers + a.per_wg - 1) / a.per_wg;
     const int64_t grid = (slices + 7) / 8 * 8 * a.q_parts;
-    if (grid > 2147483647LL) return EFANNA_EUNSUPPORTED;
+    if (grid > 2147483647LL || !launch_fits(grid, 512)) return EFANNA_EUNSUPPORTED;
     scan_wide_kernel<KS, QF><<<(unsigned)grid, 512, lds, st>>>(a);
     return EFANNA_OK;
 }
@@ -1414,9 +1420,14 @@ extern "C" int efanna_mx_quantise(const void *X, int32_t dtype, int64_t n, int32
     const int nb = mx_blocks(d), sp = mx_scale_pitch(d);
     int group = nb == 1 ? 4 : nb == 2 ? 8 : 16;      // (200 003 rows of 50 half-precision values: 8 lanes 11.7 us, 16 lanes 17.5)
     while (nb > 2 && group < 64 && group < 4 * sp) group <<= 1;
-    const int64_t blocks = (n + 256 / group - 1) / (256 / group);
-    EF_MX_DTYPE(dtype, T, (quantise_kernel<T><<<(unsigned)blocks, 256, 0, st>>>((const T *)X, n, d, ldx, group, nb, sp, codes, scales, norms)));
-    EF_HIP_CHECK(hipGetLastError());
+    const int64_t rows = 256 / group, slice = kSliceBlocks * rows;      // rows of a workgroup, of a launch
+    for (int64_t first = 0; first < n; first += slice) {
+        const int64_t here = n - first < slice ? n - first : slice;
+        EF_MX_DTYPE(dtype, T, (quantise_kernel<T><<<(unsigned)((here + rows - 1) / rows), 256, 0, st>>>(
+                                  (const T *)X + first * ldx, here, d, ldx, group, nb, sp, codes + (size_t)first * nb * 16,
+                                  scales + (size_t)first * sp, norms + first)));
+        EF_HIP_CHECK(hipGetLastError());
+    }
     return EFANNA_OK;
 }
 
@@ -1432,12 +1443,20 @@ extern "C" int efanna_mx_rows(const uint8_t *codes, const uint8_t *scales, int64
     const bool past_cache = m * d * (16 / per) > kStreamBytes;
     int group = 1;
     while (group < 64 && group * per < d) group <<= 1;
-    const int64_t rows = kRows * (256 / group), blocks = (m + rows - 1) / rows;
-    EF_MX_DTYPE(dtype, T, {
-        if (past_cache) rows_kernel<T, true><<<(unsigned)blocks, 256, 0, st>>>(t, d, ids, m, group, factor, (T *)out);
-        else rows_kernel<T, false><<<(unsigned)blocks, 256, 0, st>>>(t, d, ids, m, group, factor, (T *)out);
-    });
-    EF_HIP_CHECK(hipGetLastError());
+    const int64_t rows = kRows * (256 / group), slice = kSliceBlocks * rows;      // rows of a workgroup, of a launch
+    for (int64_t first = 0; first < m; first += slice) {
+        const int64_t here = m - first < slice ? m - first : slice;
+        const unsigned blocks = (unsigned)((here + rows - 1) / rows);
+        // (without ids the slice's rows are a table of their own)
+        const Table from = ids ? t : Table{codes + (size_t)first * t.nb * 16, scales + (size_t)first * t.sp, nullptr, (int)(n - first), t.nb, t.sp};
+        const int *slice_ids = ids ? ids + first : nullptr;
+        EF_MX_DTYPE(dtype, T, {
+            T *to = (T *)out + (size_t)first * d;
+            if (past_cache) rows_kernel<T, true><<<blocks, 256, 0, st>>>(from, d, slice_ids, here, group, factor, to);
+            else rows_kernel<T, false><<<blocks, 256, 0, st>>>(from, d, slice_ids, here, group, factor, to);
+        });
+        EF_HIP_CHECK(hipGetLastError());
+    }
     return EFANNA_OK;
 }
 

@@ -1,4 +1,5 @@
-"""MXFP4 tables at the limits that the header states: squared lengths next to the largest that have neighbours."""
+"""MXFP4 tables at the limits that the header states: squared lengths next to the largest that have neighbours, and more rows
+than one launch takes."""
 import numpy as np
 import pytest
 
@@ -62,3 +63,35 @@ def test_rows_and_queries_on_both_sides_of_the_largest_norm(ef, nq, d):
         by = np.argsort(dist, kind="stable")[:128]
         assert np.array_equal(ids[i], near[by])
         assert np.array_equal(dists[i].astype(np.float64), dist[by])
+
+
+def repeated(ef, d, n, dtype):
+    """1009 rows, their table, and for n rows which of them each is."""
+    gen = torch.Generator(device="cuda").manual_seed(d)
+    x = torch.randn((1009, d), generator=gen, device="cuda").to(dtype)
+    return x, ef.efanna_mx_quantise(x), torch.arange(n, device="cuda", dtype=torch.int32) % 1009
+
+
+def test_more_rows_than_one_launch_quantises(ef):
+    """Rows of nine blocks take a wave each: 2^25 of them and some."""
+    x, small, which = repeated(ef, 257, 2 ** 25 + 37, torch.bfloat16)
+    t = ef.efanna_mx_quantise(x[which])
+    assert torch.equal(t.norms, small.norms[which])
+    assert torch.equal(t.scales, small.scales[which])
+    assert torch.equal(t.codes, small.codes[which])
+
+
+@pytest.mark.parametrize("by_id", [True, False])
+def test_more_rows_than_one_launch_reads(ef, by_id):
+    """Sixteen rows of 257 values a workgroup: 2^27 of them and some, 69 GB."""
+    _, small, which = repeated(ef, 257, 2 ** 27 + 21, torch.bfloat16)
+    if by_id:
+        out = ef.efanna_mx_rows(small, which, factor=0.5, dtype=torch.bfloat16)
+    else:
+        table = ef.MxTable(small.codes[which], small.scales[which], small.norms[which], 257)
+        out = ef.efanna_mx_rows(table, factor=0.5, dtype=torch.bfloat16)
+    want = ef.efanna_mx_rows(small, factor=0.5, dtype=torch.bfloat16)
+    assert out.shape == (len(which), 257)
+    step = 2 ** 24
+    for at in range(0, len(which), step):
+        assert torch.equal(out[at:at + step], want[which[at:at + step]])
