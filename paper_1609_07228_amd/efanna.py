@@ -113,9 +113,14 @@ def _dev(t: torch.Tensor, dtype) -> torch.Tensor:
     return t
 
 
-def _workspace(nbytes: int, device) -> torch.Tensor:
-    # torch's caching allocator hands out 512-byte aligned blocks
-    return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
+def _workspace(nbytes: int, on: torch.Tensor, given: torch.Tensor | None) -> torch.Tensor:
+    """`given`, or else a new workspace, on the GPU that holds `on`."""
+    if given is None:
+        # torch's caching allocator hands out 512-byte aligned blocks
+        return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=on.device)
+    if given.get_device() != on.get_device() or not given.is_contiguous():
+        raise ValueError("the workspace is not a contiguous tensor on the GPU of the other tensors")
+    return given
 
 
 NODE_BYTES = 32      # sizeof(efanna_node): int64 sum; int32 dim, cnt, parent, depth, child[2]
@@ -153,7 +158,7 @@ def efanna_build_trees(X: torch.Tensor, n_trees: int, leaf_size: int, seed: int,
         leaf_up = torch.full((n_trees, max_leaves + 1), -1, dtype=torch.int32, device=X.device)
     depth = C.c_int32(-1)
     need = lib().efanna_trees_workspace_bytes(n, d, n_trees, leaf_size, 1 if with_nodes else 0)
-    ws = _workspace(need, X.device) if workspace is None else workspace
+    ws = _workspace(need, X, workspace)
     tail = (perm.data_ptr(), leaf_off.data_ptr(), max_leaves, n_leaves.ctypes.data_as(C.c_void_p),
             nodes.data_ptr() if with_nodes else None, leaf_up.data_ptr() if with_nodes else None,
             C.byref(depth), ws.data_ptr(), ws.numel())
@@ -191,7 +196,7 @@ def efanna_init_graph(X: torch.Tensor, perm: torch.Tensor, leaf_off: torch.Tenso
         graph = torch.empty((n, k), dtype=torch.int64, device=X.device)
     levels = 0 if nodes is None else int(tree_depth) - int(conquer_depth) + 1
     need = lib().efanna_init_workspace_bytes(n, levels)
-    ws = _workspace(need, X.device) if workspace is None else workspace
+    ws = _workspace(need, X, workspace)
     _call("efanna_init_graph", X, X.data_ptr(), n, d, perm.data_ptr(), leaf_off.data_ptr(),
           leaf_off.shape[1] - 1, n_leaves.ctypes.data_as(C.c_void_p),
           nodes.data_ptr() if nodes is not None else None,
@@ -221,7 +226,7 @@ def efanna_nndescent(X: torch.Tensor, graph: torch.Tensor, iters: int, sample_L:
     if phase_ms is not None:
         assert phase_ms.dtype == np.float32 and phase_ms.size >= 4 * iters and phase_ms.flags.c_contiguous
     need = lib().efanna_nndescent_workspace_bytes(n, k, sample_L)
-    ws = _workspace(need, X.device) if workspace is None else workspace
+    ws = _workspace(need, X, workspace)
     done = C.c_int32(0)
     _call("efanna_nndescent", X, X.data_ptr(), n, d, k, graph.data_ptr(), iters, sample_L, seed,
           first_iter, float(delta), 1 if cross_old else 0, C.byref(done), stats.data_ptr(),
@@ -304,7 +309,7 @@ def efanna_search(X: torch.Tensor, perm: torch.Tensor, leaf_off: torch.Tensor, n
     dists = torch.empty((nq, k), dtype=torch.float32, device=X.device)
     checked = torch.empty((nq,), dtype=torch.int32, device=X.device)
     need = lib().efanna_search_workspace_bytes(nq, d, T, leaf_size, tree_depth, g.shape[1], pool, iters)
-    ws = _workspace(need, X.device) if workspace is None else workspace
+    ws = _workspace(need, X, workspace)
     _call("efanna_search", X, X.data_ptr(), n, d, perm.data_ptr(), leaf_off.data_ptr(),
           leaf_off.shape[1] - 1, n_leaves.ctypes.data_as(C.c_void_p),
           nodes.data_ptr(), int(tree_depth), T, leaf_size, g.data_ptr(), g.shape[1],
@@ -414,7 +419,7 @@ def efanna_mx_nearest(table: MxTable, queries: MxTable, k: int, first_self: int 
     device = table.codes.device
     ids = torch.empty((nq, max(k, 0)), dtype=torch.int32, device=device)
     dists = torch.empty((nq, max(k, 0)), dtype=torch.float32, device=device)
-    ws = _workspace(lib().efanna_mx_nearest_workspace_bytes(n, table.d, nq, k), device) if workspace is None else workspace
+    ws = _workspace(lib().efanna_mx_nearest_workspace_bytes(n, table.d, nq, k), table.codes, workspace)
     _call("efanna_mx_nearest", table.codes, table.codes.data_ptr(), table.scales.data_ptr(), table.norms.data_ptr(), n,
           table.d, queries.codes.data_ptr(), queries.scales.data_ptr(), queries.norms.data_ptr(), nq, k,
           int(first_self), ids.data_ptr(), dists.data_ptr(), ws.data_ptr(), ws.numel())

@@ -1,5 +1,5 @@
-"""On which GPU and stream the binding's calls run, without a GPU: CPU tensors that say that they lie on GPU 1, a
-library that notes the current GPU and the stream it is given, and GPU 0 current."""
+"""On which GPU and stream the binding's calls run and which workspaces they take, without a GPU: CPU tensors that say
+that they lie on GPU 1, a library that notes the current GPU and the stream it is given, and GPU 0 current."""
 import numpy as np
 import pytest
 
@@ -95,3 +95,34 @@ def test_runs_on_the_gpu_of_its_tensors(calls, name, here):
     CALLS[name](efanna)
     assert made == [(name, 1, stream_of(1))]
     assert current[0] == here
+
+
+TAKES_WORKSPACE = {
+    "efanna_build_trees": lambda ef, ws: ef.efanna_build_trees(gpu1(9, 4), 2, 4, 0, workspace=ws),
+    "efanna_init_graph": lambda ef, ws: ef.efanna_init_graph(gpu1(9, 4), gpu1(2, 9, dtype=torch.int32),
+                                                             gpu1(2, 10, dtype=torch.int32), np.ones(2, np.int32), 4, 3,
+                                                             workspace=ws),
+    "efanna_nndescent": lambda ef, ws: ef.efanna_nndescent(gpu1(9, 4), gpu1(9, 3, dtype=torch.int64), 1, 4, 0, workspace=ws),
+    "efanna_search": lambda ef, ws: ef.efanna_search(gpu1(9, 4), gpu1(2, 9, dtype=torch.int32), gpu1(2, 10, dtype=torch.int32),
+                                                     np.ones(2, np.int32), gpu1(2, 10, 32, dtype=torch.uint8), 1, 4,
+                                                     gpu1(9, 3, dtype=torch.int32), gpu1(2, 4), 1, 4, 2, 1, workspace=ws),
+    "efanna_mx_nearest": lambda ef, ws: ef.efanna_mx_nearest(table(ef), table(ef), 2, workspace=ws),
+}
+
+
+class OnGpu0(OnGpu1):
+    def get_device(self):
+        return 0
+
+
+@pytest.mark.parametrize("name", TAKES_WORKSPACE)
+def test_workspace_lies_with_the_tensors_and_in_one_piece(calls, name):
+    """A kernel would write wherever the pointer leads: host memory, another GPU, or what lies between a view's elements."""
+    efanna, made, _ = calls
+    room = torch.zeros(4096, dtype=torch.uint8)
+    for bad in (room, room.as_subclass(OnGpu0), room.as_subclass(OnGpu1)[::2]):
+        with pytest.raises(ValueError):
+            TAKES_WORKSPACE[name](efanna, bad)
+    assert made == []
+    TAKES_WORKSPACE[name](efanna, room.as_subclass(OnGpu1))
+    assert len(made) == 1
