@@ -420,7 +420,10 @@ def efanna_mx_nearest(table: MxTable, queries: MxTable, k: int, first_self: int 
     ids = torch.empty((nq, max(k, 0)), dtype=torch.int32, device=device)
     dists = torch.empty((nq, max(k, 0)), dtype=torch.float32, device=device)
     ws = _workspace(lib().efanna_mx_nearest_workspace_bytes(n, table.d, nq, k), table.codes, workspace)
-    _call("efanna_mx_nearest", table.codes, table.codes.data_ptr(), table.scales.data_ptr(), table.norms.data_ptr(), n,
+    norms = table.norms
+    if norms.data_ptr() & 15:         # (a table cut out of another from a row on that four does not divide)
+        norms = norms.clone()
+    _call("efanna_mx_nearest", table.codes, table.codes.data_ptr(), table.scales.data_ptr(), norms.data_ptr(), n,
           table.d, queries.codes.data_ptr(), queries.scales.data_ptr(), queries.norms.data_ptr(), nq, k,
           int(first_self), ids.data_ptr(), dists.data_ptr(), ws.data_ptr(), ws.numel())
     return ids, dists

@@ -1,5 +1,6 @@
-"""On which GPU and stream the binding's calls run and which workspaces they take, without a GPU: CPU tensors that say
-that they lie on GPU 1, a library that notes the current GPU and the stream it is given, and GPU 0 current."""
+"""On which GPU and stream the binding's calls run, which workspaces they take and what they hand over of a table cut out of
+another, without a GPU: CPU tensors that say that they lie on GPU 1, a library that notes the current GPU and the stream it is
+given, and GPU 0 current."""
 import numpy as np
 import pytest
 
@@ -126,3 +127,20 @@ def test_workspace_lies_with_the_tensors_and_in_one_piece(calls, name):
     assert made == []
     TAKES_WORKSPACE[name](efanna, room.as_subclass(OnGpu1))
     assert len(made) == 1
+
+
+@pytest.mark.parametrize("first", range(6))
+def test_norms_of_a_table_cut_from_any_row(calls, monkeypatch, first):
+    """The entry point asks for norms at a multiple of 16 bytes; codes and scales are at one from any row on."""
+    efanna, _, _ = calls
+    import ctypes
+    seen = []
+
+    def call(name, on, codes, scales, norms, n, *rest):
+        seen.append((codes, scales, norms % 16, list((ctypes.c_float * n).from_address(norms))))
+    monkeypatch.setattr(efanna, "_call", call)
+    whole = efanna.MxTable(gpu1(9, 32, dtype=torch.uint8), gpu1(9, 4, dtype=torch.uint8),
+                           torch.arange(9, dtype=torch.float32).as_subclass(OnGpu1), 40)
+    cut = efanna.MxTable(whole.codes[first:], whole.scales[first:], whole.norms[first:], 40)
+    efanna.efanna_mx_nearest(cut, whole, 2)
+    assert seen == [(cut.codes.data_ptr(), cut.scales.data_ptr(), 0, [float(i) for i in range(first, 9)])]

@@ -95,3 +95,21 @@ def test_more_rows_than_one_launch_reads(ef, by_id):
     step = 2 ** 24
     for at in range(0, len(which), step):
         assert torch.equal(out[at:at + step], want[which[at:at + step]])
+
+
+@pytest.mark.parametrize("first", [1, 2, 3, 4, 5])
+@pytest.mark.parametrize("nq", [3, 100])
+def test_a_table_cut_from_any_row(ef, first, nq):
+    """Every operator on rows `first` and on of a table, as views of it, and on a table of those rows alone."""
+    gen = torch.Generator(device="cuda").manual_seed(first + nq)
+    x = torch.randn((1000, 70), generator=gen, device="cuda")
+    whole, alone = ef.efanna_mx_quantise(x), ef.efanna_mx_quantise(x[first:])
+    cut = ef.MxTable(whole.codes[first:], whole.scales[first:], whole.norms[first:], 70)
+    q = ef.efanna_mx_quantise(torch.randn((nq, 70), generator=gen, device="cuda"))
+    for got, want in zip(ef.efanna_mx_nearest(cut, q, 9), ef.efanna_mx_nearest(alone, q, 9)):
+        assert torch.equal(got, want)
+    for got, want in zip(ef.efanna_mx_nearest(q, cut, 2), ef.efanna_mx_nearest(q, alone, 2)):
+        assert torch.equal(got, want)
+    assert torch.equal(ef.efanna_mx_rows(cut), ef.efanna_mx_rows(alone))
+    assert torch.equal(ef.efanna_mx_product(q, cut), ef.efanna_mx_product(q, alone))
+    assert torch.equal(ef.efanna_mx_product(cut, q), ef.efanna_mx_product(alone, q))
