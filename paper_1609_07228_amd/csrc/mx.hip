@@ -934,6 +934,7 @@ __global__ __launch_bounds__(256, 2) void scan_narrow_kernel(Scan a)
 #pragma unroll 1
             for (int tile = 0; tile < TS; ++tile) pass(std::false_type(), tile);
         }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // (read before it is written again)
     }
 #pragma unroll
     for (int f = 0; f < QF; ++f) {

@@ -1,5 +1,5 @@
-"""MXFP4 tables at the limits that the header states: squared lengths next to the largest that have neighbours, and more rows
-than one launch takes."""
+"""MXFP4 tables at the limits that the header states: squared lengths next to the largest that have neighbours, more rows
+than one launch takes; and long tables, whose groups of rows are so large that a wave takes them in several rounds."""
 import numpy as np
 import pytest
 
@@ -113,3 +113,22 @@ def test_a_table_cut_from_any_row(ef, first, nq):
     assert torch.equal(ef.efanna_mx_rows(cut), ef.efanna_mx_rows(alone))
     assert torch.equal(ef.efanna_mx_product(q, cut), ef.efanna_mx_product(q, alone))
     assert torch.equal(ef.efanna_mx_product(cut, q), ef.efanna_mx_product(alone, q))
+
+
+@pytest.mark.parametrize("n,d", [(250_003, 16), (262_144, 128), (110_001, 200), (440_001, 256), (300_007, 500), (75_003, 600),
+                                 (292_001, 640), (130_001, 896), (125_009, 1000), (492_007, 1024)])
+@pytest.mark.parametrize("nq", [1, 40, 130, 600])
+def test_groups_of_rows_that_take_several_rounds(ef, n, d, nq):
+    """The shapes next above those from which groups of 32, 64 and 128 rows are taken for one neighbour."""
+    gen = torch.Generator(device="cuda").manual_seed(n + nq)
+    x = torch.randint(-2, 3, (n, d), generator=gen, device="cuda").to(torch.float32)
+    y = torch.randint(-2, 3, (nq, d), generator=gen, device="cuda").to(torch.float32)
+    x[:, ::32], y[:, ::32] = 4.0, 4.0                    # every block's scale is 1
+    t, q = ef.efanna_mx_quantise(x), ef.efanna_mx_quantise(y)
+    xx = x.square().sum(dim=1)
+    for _ in range(2):
+        ids, dists = ef.efanna_mx_nearest(t, q, 1)
+        for at in list(range(min(nq, 40))) + [nq - 1]:
+            dist = (xx - 2.0 * (x @ y[at]) + y[at].square().sum()).to(torch.float64)       # whole numbers below 2^24
+            want = (dist * 2 ** 20 + torch.arange(n, device="cuda")).argmin()
+            assert ids[at, 0] == want and dists[at, 0] == dist[want]
