@@ -341,7 +341,7 @@ int efanna_mx_product(const uint8_t *a_codes, const uint8_t *a_scales, int64_t m
 /* For each of nq rows q of one table the k rows x of another that come first in the order
  * (s descending, id ascending), s = q.x - |x|^2 / 2 in float32 with |x|^2 taken from norms.
  * That is the order (squared distance, id) of the rows as held, up to the rounding of s; s is exact
- * wherever the terms of a sum span no more than 24 bits.
+ * wherever the terms of a sum span no more than 24 bits and are multiples of 2^-149.
  * norms, q_norms [device] as efanna_mx_quantise writes them (norms 16-byte aligned).  Only norms below
  *        EFANNA_MX_MAX_NORM take part, so that no sum and no distance leaves the float32 range: a row
  *        of a larger norm, or of none (NaN), is nobody's neighbour, and such a query has none.

@@ -132,3 +132,21 @@ def test_groups_of_rows_that_take_several_rounds(ef, n, d, nq):
             dist = (xx - 2.0 * (x @ y[at]) + y[at].square().sum()).to(torch.float64)       # whole numbers below 2^24
             want = (dist * 2 ** 20 + torch.arange(n, device="cuda")).argmin()
             assert ids[at, 0] == want and dists[at, 0] == dist[want]
+
+
+@pytest.mark.parametrize("power", [-55, -63, -66, -73])
+@pytest.mark.parametrize("m,n,d", [(3, 300, 64), (300, 301, 256), (20, 100, 1100)])
+def test_products_below_the_normal_range(ef, power, m, n, d):
+    """Small whole multiples of a power whose square is subnormal or next to it: nothing is lost above 2^-149."""
+    gen = torch.Generator(device="cuda").manual_seed(n + d)
+    x = torch.randint(-2, 3, (m, d), generator=gen, device="cuda").to(torch.float64)
+    y = torch.randint(-2, 3, (n, d), generator=gen, device="cuda").to(torch.float64)
+    x[:, ::32], y[:, ::32] = 4.0, 4.0
+    a, b = (ef.efanna_mx_quantise((v * 2.0 ** power).to(torch.float32)) for v in (x, y))
+    product = x @ y.T
+    assert torch.equal(ef.efanna_mx_product(a, b).to(torch.float64), product * 2.0 ** (2 * power))
+    dist = x.square().sum(dim=1, keepdim=True) + y.square().sum(dim=1) - 2 * product
+    want = (dist * 4096 + torch.arange(n, device="cuda")).topk(7, dim=1, largest=False).indices
+    ids, dists = ef.efanna_mx_nearest(b, a, 7)
+    assert torch.equal(ids.to(torch.int64), want)
+    assert torch.equal(dists.to(torch.float64), dist.gather(1, want) * 2.0 ** (2 * power))
