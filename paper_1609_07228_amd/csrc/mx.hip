@@ -89,7 +89,8 @@ template <int CTRL> __device__ inline float mx_from(float x) { return __uint_as_
 // ---- quantisation ----------------------------------------------------------------------------------------
 // Four lanes per block, eight coordinates each; a row's lanes are `group` consecutive ones (4 for a row of one block, 8 for two,
 // else a power of two from 16 on), so a wave holds 64 / group rows and the row's squared length is a sum over those lanes.
-// Bound: HBM for rows that fill their lanes (10^6 x 128 float32, 590 MB: 103 us, 5.7 TB/s), instructions for short ones.
+// Bound: HBM for rows that fill their lanes (10^6 x 128 float32, 590 MB: 103 us, 5.7 TB/s), instructions for short ones (200 003 x
+// 50 half precision: 11.8 us, vector instructions for 0.73 of it).
 template <class T>
 __global__ __launch_bounds__(256) void quantise_kernel(const T *X, long long n, int d, long long ldx, int group, int nb,
                                                        int sp, uint8_t *codes, uint8_t *scales, float *norms)
@@ -140,8 +141,9 @@ __global__ __launch_bounds__(256) void quantise_kernel(const T *X, long long n, 
 
 // ---- rows by id ------------------------------------------------------------------------------------------
 // A lane per 16 bytes of an output row (4 or 8 coordinates: neighbouring lanes' stores touch), `group` lanes (a power of two)
-// per row and kRows rows per lane, so that as many chains of id, codes, store run side by side.  Bound: HBM writes (2 * 10^6 rows of
-// 128 by id to bf16, 512 MB: 92 us, 5.6 TB/s; 10^6 rows to float32: 91 us, 6.4 TB/s with the table).  Codes have two significant
+// per row and kRows rows per lane, so that as many chains of id, codes, store run side by side.  Bound: HBM writes (10^6 rows of 128
+// to float32: 91 us, 6.4 TB/s with the table), and instructions for 16-bit outputs (2 * 10^6 rows by id to bf16, 512 MB: 92 us,
+// 5.6 TB/s, vector instructions for 0.94 of the time).  Codes have two significant
 // bits, so value * scale is exact; the factor's product is rounded to float32 and then once to the output's type.
 constexpr int kRows = 4;
 template <class T, bool PAST_CACHE>
@@ -248,11 +250,12 @@ template <int N> __device__ inline void wait_loads() { asm volatile("s_waitcnt v
 // coordinates of both, whole lines of 128 bytes (half lines cost the loads as much each), and the scales of 512 coordinates
 // with every other one; while one is computed the next is on its way into LDS.  A load of codes brings 8 rows; the blocks of row
 // r lie in the order b ^ (r / 2) % 8, so that blocks b of 16 rows, which are read together, are in different ones of the 64 banks.
-// Bound: clocks under load, then what a stage waits for.  8192^3 takes 0.28 ms, 3.9 PFLOP/s, at 1.7 GHz with the matrix units busy for
-// 0.54 and LDS for 0.33 of the time; all loads from the same eight rows (less to move and fewer bits that change) 0.24.
+// Bound: what a stage waits for, all eight waves at its one barrier, and clocks under load.  8192^3 takes 0.28 ms, 3.9 PFLOP/s, at
+// 1.74 GHz with the matrix units busy for 0.55 and LDS for 0.34 of the time (a fifth of that are conflicts); all loads from the same
+// eight rows (less to move and fewer bits that change) 0.24.
 // Tiles of 128 x 128, two workgroups a CU, 0.36: they load twice as much.  Long outputs of short sums wait for their stores too:
-// 4096 x 65536 x 960 to bf16 0.26 ms, of which 0.1 go with the stores; workgroups that stay and ask for the next tile before they
-// store this one were no faster, and 0.27 with stores past the caches.
+// 4096 x 65536 x 960 to bf16 0.27 ms, without its stores 0.16; workgroups that stay and ask for the next tile before they store
+// this one were no faster, and 0.27 with stores past the caches.
 template <int FA, int FB, int WA, int WB>
 struct Tiling {
     static constexpr int waves = WA * WB, side_a = 32 * FA * WA, side_b = 32 * FB * WB, sides = side_a + side_b;
@@ -789,9 +792,12 @@ __device__ inline f32x4 mx_start(const Lds *l, int tile, int g, int left)
 }
 
 // Many queries: a workgroup of 8 waves holds 8 * QF * 16 queries in registers and passes the rows of its supers
-// through LDS, a stage of about kStage operands at a time, loaded while the stage before is computed.  Bound: clocks under load
-// (10 000 queries of 10^6 x 128: 0.56 ms, 4.6 PFLOP/s, the matrix units busy for 0.57 of the time at 1.9 GHz and other vector
-// instructions, two minima per matrix instruction most of all, for as much; 1000 of 10^6 x 960: 0.43 ms, 4.5 PFLOP/s).
+// through LDS, a stage of about kStage operands at a time; the next one is asked for before this one is computed.  10 000 queries of
+// 10^6 x 128 take 0.57 ms, 4.5 PFLOP/s, at 1.9 GHz: matrix units busy for 0.57 of the time, other vector instructions, two minima per
+// matrix instruction most of all, for 0.44.  <1, 8>, which is what they take, has seven values more than its 128 registers hold; four
+// are read back in every stage behind the next stage's loads, and the wait for them is one for those loads too, so that in this variant
+// loads and computation take turns within a wave (the other workgroup of the CU goes on).  1000 of 10^6 x 960: 0.45 ms, 4.3 PFLOP/s, at
+// 2.0 GHz, matrix units busy for 0.56: a step's operand is read from LDS right before its matrix instructions, which wait for it.
 constexpr int kStage = 32;
 
 template <int KS, int QF>
@@ -885,7 +891,8 @@ __global__ __launch_bounds__(512, KS == 1 ? 4 : 2) void scan_wide_kernel(Scan a)
 }
 
 // Few queries: all four waves of a workgroup hold the same QF * 16 of them and take a block of a super each, up to 16
-// operands of it in flight.  Bound by HBM: the rows are read once (one query of 10^6 x 128, 72 MB: 14.5 us, 5.0 TB/s).
+// operands of it in flight.  Bound by HBM: the rows are read once (one query of 10^6 x 128, 72 MB: 14.7 us, 4.9 TB/s).  (<7, 4> has
+// ten values more than its registers hold; the choice below counts that in.)
 template <int KS, int QF>
 __global__ __launch_bounds__(256, 2) void scan_narrow_kernel(Scan a)
 {
