@@ -1,5 +1,5 @@
-"""Products of MXFP4 tables with more tiles than run at once: workgroups go from tile to tile, and the next tile's first loads
-pass the stores of the one before.  Coordinates are whole numbers that the format holds, so every output is known exactly."""
+"""Products of MXFP4 tables with more tiles than run at once, a workgroup for each, with sums of one stage to several and remainders
+in every direction.  Coordinates are whole numbers that the format holds, so every output is known exactly."""
 import pytest
 
 torch = pytest.importorskip("torch")
