@@ -333,7 +333,9 @@ int efanna_mx_rows(const uint8_t *codes, const uint8_t *scales, int64_t n, int32
                    int64_t m, float factor, int32_t dtype, void *out, void *stream);
 
 /* out[i * ldo + j] = a_i . b_j for the m rows of one table and the n rows of another, ldo >= n.
- * Summed in float32 by the matrix units, rounded once to dtype. */
+ * Summed in float32 by the matrix units, rounded once to dtype.  EFANNA_EUNSUPPORTED for what one
+ * launch does not take: 2^23 tiles of 256 x 256 and more (half a terabyte of output), or up to 32 rows
+ * against 2^30 and more of above 896 coordinates (half a terabyte of table). */
 int efanna_mx_product(const uint8_t *a_codes, const uint8_t *a_scales, int64_t m, const uint8_t *b_codes,
                       const uint8_t *b_scales, int64_t n, int32_t d, int32_t dtype, void *out, int64_t ldo,
                       void *stream);
