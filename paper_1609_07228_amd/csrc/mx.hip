@@ -9,69 +9,22 @@
 // A block is what one lane hands v_mfma_scale_f32_16x16x128_f8f6f4 as its part of an operand: lane l holds
 // block 4 s + l / 16 of row l % 16 in step s, and its scale byte.  Row-major codes are therefore operands
 // without any rearrangement, 16 bytes per lane and step.  The unit multiplies exactly and adds in float32.
-#include "common.h"
+#include "tables.h"
 
-#include <stdint.h>
 #include <type_traits>
 
 namespace {
 
-typedef int i32x4 __attribute__((ext_vector_type(4)));
-typedef int i32x8 __attribute__((ext_vector_type(8)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-
 constexpr int kFp4 = 4;                    // the operand format's number in the matrix instruction
-// Outputs larger than the L2 caches are stored past them (10^6 x 128 float32 read back: 102 -> 81 us); smaller ones are left there
-// for whoever reads them next.
-constexpr int64_t kStreamBytes = (int64_t)32 << 20;
 constexpr size_t kMaxWorkspace = (size_t)1 << 30;
-// A launch takes fewer than 2^32 threads.  Rows that a kernel takes one by one go in slices of so many workgroups of 256.
-constexpr int64_t kSliceBlocks = (int64_t)1 << 23;
-inline bool launch_fits(int64_t blocks, int64_t threads) { return blocks <= 4294967295LL / threads; }
-
-// (64 KiB and less need no leave, and asking for it takes a microsecond)
-inline hipError_t allow_lds(const void *kernel, int bytes)
-{
-    return bytes > 65536 ? hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) : hipSuccess;
-}
 __host__ __device__ inline int mx_blocks(int d) { return (d + 31) >> 5; }
 __host__ __device__ inline int mx_scale_pitch(int d) { return (mx_blocks(d) + 3) & ~3; }
-inline size_t align_up(size_t x) { return (x + 255) & ~(size_t)255; }
-
 struct Table {
     const uint8_t *codes, *scales;
     const float *norms;
     int n, nb, sp;
 };
 
-// 2^(b - 127); 255 stands for NaN
-__device__ inline float mx_scale(u32 b)
-{
-    return __uint_as_float(b == 0 ? 0x00400000u : b == 255 ? 0x7FC00000u : b << 23);
-}
-
-// ---- element types -------------------------------------------------------------------------------------
-template <class T> __device__ inline float to_float(T x) { return (float)x; }
-template <class T> __device__ inline T from_float(float x) { return (T)x; }      // to nearest, ties to even
-
-// Eight values from or to any address that suits the element (the last ones of a row: fewer).
-template <class T>
-__device__ inline void load_eight(const T *p, int left, float (&v)[8])
-{
-    typedef T Piece __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
-    constexpr int kPer = 16 / sizeof(T);
-    if (left >= 8) {
-#pragma unroll
-        for (int i = 0; i < 8; i += kPer) {
-            const Piece x = *(const Piece *)(p + i);
-#pragma unroll
-            for (int j = 0; j < kPer; ++j) v[i + j] = to_float(x[j]);
-        }
-    } else
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = j < left ? to_float(p[j]) : 0.0f;
-}
 // the eight values of a word of codes
 __device__ inline void mx_values(u32 word, float scale, float (&v)[8])
 {
@@ -79,12 +32,6 @@ __device__ inline void mx_values(u32 word, float scale, float (&v)[8])
     const f32x2 h2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, scale, 2), h3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, scale, 3);
     v[0] = h0.x, v[1] = h0.y, v[2] = h1.x, v[3] = h1.y, v[4] = h2.x, v[5] = h2.y, v[6] = h3.x, v[7] = h3.y;
 }
-
-// A neighbour's value by row operations (no trip through LDS): the other lane of a pair, of a pair of pairs; the lane 4 or
-// 8 further within a row of 16, around its end.
-constexpr int kSwap1 = 0xB1, kSwap2 = 0x4E, kDown4 = 0x120 + 12, kDown8 = 0x120 + 8;
-template <int CTRL> __device__ inline u32 mx_from(u32 x) { return (u32)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true); }
-template <int CTRL> __device__ inline float mx_from(float x) { return __uint_as_float(mx_from<CTRL>(__float_as_uint(x))); }
 
 // ---- quantisation ----------------------------------------------------------------------------------------
 // Four lanes per block, eight coordinates each; a row's lanes are `group` consecutive ones (4 for a row of one block, 8 for two,
@@ -108,12 +55,12 @@ __global__ __launch_bounds__(256) void quantise_kernel(const T *X, long long n, 
         u32 top = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[j]) & 0x7FFFFFFFu);
-        top = max(top, mx_from<kSwap1>(top));
-        top = max(top, mx_from<kSwap2>(top));
+        top = max(top, lane_from<kSwap1>(top));
+        top = max(top, lane_from<kSwap2>(top));
         const u32 e = top >> 23;
         const bool bad = e == 255;
         const u32 b = bad ? 255u : e > 2 ? e - 2 : 0u;
-        const float scale = mx_scale(bad ? 127 : b);
+        const float scale = scale_value(bad ? 127 : b);
         u32 word = 0;
         word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[0], v[1], scale, 0);
         word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[2], v[3], scale, 1);
@@ -124,17 +71,17 @@ __global__ __launch_bounds__(256) void quantise_kernel(const T *X, long long n, 
         if (block < nb) *(u32 *)(row_codes + (size_t)p * 4) = word;
         // four blocks' scales as a word
         u32 four = block < nb ? b : 0;
-        if (group > 4) four |= mx_from<kDown4>(four) << 8;
-        if (group > 8) four |= mx_from<kDown8>(four) << 16;
+        if (group > 4) four |= lane_from<kDown4>(four) << 8;
+        if (group > 8) four |= lane_from<kDown8>(four) << 16;
         if ((p & 15) == 0) *(u32 *)(row_scales + block) = four;
         mx_values(word, scale, v);
         norm += (v[0] * v[0] + v[1] * v[1]) + (v[2] * v[2] + v[3] * v[3]) + (v[4] * v[4] + v[5] * v[5]) + (v[6] * v[6] + v[7] * v[7]);
         if (bad) norm = __uint_as_float(0x7FC00000u);
     }
-    norm += mx_from<kSwap1>(norm);
-    norm += mx_from<kSwap2>(norm);
-    if (group > 4) norm += mx_from<kDown4>(norm);
-    if (group > 8) norm += mx_from<kDown8>(norm);
+    norm += lane_from<kSwap1>(norm);
+    norm += lane_from<kSwap2>(norm);
+    if (group > 4) norm += lane_from<kDown4>(norm);
+    if (group > 8) norm += lane_from<kDown8>(norm);
     for (int o = 16; o < group; o <<= 1) norm += __shfl_xor(norm, o);
     if (lane == 0) norms[row] = norm;
 }
@@ -174,7 +121,7 @@ __global__ __launch_bounds__(256) void rows_kernel(Table t, int d, const int *id
             const long long row = first + (long long)i * per;
             float v[8];
             mx_values(kPer == 4 ? word[i] >> (16 * (p & 1)) : word[i], 1.0f, v);
-            const float scale = mx_scale(b[i] & 255);
+            const float scale = scale_value(b[i] & 255);
             Piece x;
 #pragma unroll
             for (int j = 0; j < kPer; ++j) x[j] = from_float<T>(b[i] > 255 ? 0.0f : v[j] * scale * factor);
@@ -213,21 +160,12 @@ __device__ inline f32x4 mx_mma(const Operand &a, const Operand &b, f32x4 c)
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a8, b8, c, kFp4, kFp4, 0, a.scale, 0, b.scale);
 }
 
-typedef __attribute__((address_space(3))) void lds_void;
-typedef __attribute__((address_space(1))) const void global_void;
-
 // Rows pass through LDS by loads that write there directly.  An operand (16 rows, a step's 4 blocks) is 1 KiB; lane l of
 // its load brings a 16-byte block of row l / 4, so that four lanes share 64 consecutive bytes of memory (with the lanes in the
 // order the matrix instruction wants them the loads return a quarter as fast).  The blocks of row r lie in the order
 // b ^ (r / 2) % 4, so that blocks b of eight neighbouring rows, which are read together, are in different banks.
 __device__ inline int mx_stage_block(int lane, int step, int nb) { return min(4 * step + ((lane & 3) ^ ((lane >> 3) & 3)), nb - 1); }
 __device__ inline int mx_staged_at(int r, int g) { return (r * 4 + (g ^ ((r >> 1) & 3))) * 4; }      // word within the operand
-__device__ inline void mx_stage(const void *from, void *to, int lane_bytes_16)
-{
-    if (lane_bytes_16) __builtin_amdgcn_global_load_lds((global_void *)from, (lds_void *)to, 16, 0, 0);
-    else __builtin_amdgcn_global_load_lds((global_void *)from, (lds_void *)to, 4, 0, 0);
-}
-
 // ---- product ---------------------------------------------------------------------------------------------
 // out[i][j] = a_i . b_j.  The rows of b are the instruction's rows and those of a its columns, so that a lane
 // ends up with four consecutive values of an output row.
@@ -242,9 +180,6 @@ __device__ inline void store_four(T *o, f32x4 x, int left)
         for (int c = 0; c < 4; ++c)
             if (c < left) o[c] = from_float<T>(x[c]);
 }
-
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-template <int N> __device__ inline void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
 // WA x WB waves share a tile of a's rows by b's rows, FA x FB instructions of 32 x 32 x 64 each.  A stage is 256
 // coordinates of both, whole lines of 128 bytes (half lines cost the loads as much each), and the scales of 512 coordinates
@@ -303,14 +238,14 @@ __global__ __launch_bounds__(64 * WA * WB, FA * FB > 8 ? 1 : 2) void product_til
 #pragma unroll
         for (int i = 0; i < Tile::each; ++i) {
             const int op = wave * Tile::each + i;
-            mx_stage((op * 8 < Tile::side_a ? codes_a : codes_b) + at_codes[i] + block[i & 1], &lds.codes[stage & 1][op][0], 1);
+            stage_lds((op * 8 < Tile::side_a ? codes_a : codes_b) + at_codes[i] + block[i & 1], &lds.codes[stage & 1][op][0], 1);
         }
         if (!with_scales) return;
         const u32 word = min(8 * stage + 4 * (lane & 3), a.sp - 4);
 #pragma unroll
         for (int i = 0; i < Tile::each_scales; ++i) {
             const int op = wave * Tile::each_scales + i;
-            mx_stage((op * 16 < Tile::side_a ? scales_a : scales_b) + at_scales[i] + word, &lds.scales[(stage >> 1) & 1][op * 16][0], 0);
+            stage_lds((op * 16 < Tile::side_a ? scales_a : scales_b) + at_scales[i] + word, &lds.scales[(stage >> 1) & 1][op * 16][0], 0);
         }
     };
     f32x16 acc[FA][FB] = {};
@@ -473,8 +408,8 @@ __global__ __launch_bounds__(64 * WAVES) void product_few_kernel(Table a, Table 
             if (S > 1 && s0 + s >= s_hi) break;
             const u32 block = mx_stage_block(lane, s0 + s, b.nb) * 16;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) mx_stage(from_codes + at_codes[i] + block, &lds->codes[s * 4 + i][0], 1);
-            mx_stage(lane_scales + 4 * (s0 + s), &lds->scales[s][0][0], 0);
+            for (int i = 0; i < 4; ++i) stage_lds(from_codes + at_codes[i] + block, &lds->codes[s * 4 + i][0], 1);
+            stage_lds(lane_scales + 4 * (s0 + s), &lds->scales[s][0][0], 0);
         }
         Operand y[S][M];
 #pragma unroll
@@ -742,18 +677,18 @@ struct StageLds {
         for (int i = 0; i < (ops + WAVES - 1) / WAVES; ++i) {
             const int op = wave + WAVES * i;
             if (WAVES * (i + 1) <= ops || op < ops)
-                mx_stage(t.codes + ((size_t)row_of(op / KS, lane >> 2) * t.nb + mx_stage_block(lane, op % KS, t.nb)) * 16,
+                stage_lds(t.codes + ((size_t)row_of(op / KS, lane >> 2) * t.nb + mx_stage_block(lane, op % KS, t.nb)) * 16,
                          &codes[op][0], 1);
         }
 #pragma unroll
         for (int i = 0; i < ((ops + 3) / 4 + WAVES - 1) / WAVES; ++i) {
             const int op = (wave + WAVES * i) * 4 + g;
-            if (op < ops) mx_stage(t.scales + (size_t)row_of(op / KS, r) * t.sp + 4 * (op % KS), &scales[(wave + WAVES * i) * 4][0], 0);
+            if (op < ops) stage_lds(t.scales + (size_t)row_of(op / KS, r) * t.sp + 4 * (op % KS), &scales[(wave + WAVES * i) * 4][0], 0);
         }
 #pragma unroll
         for (int i = 0; i < ((TILES + 3) / 4 + WAVES - 1) / WAVES; ++i) {
             const int tile = (wave + WAVES * i) * 4 + g;
-            if (tile < TILES) mx_stage(t.norms + row_of(tile, r), &norms[(wave + WAVES * i) * 4][0], 0);
+            if (tile < TILES) stage_lds(t.norms + row_of(tile, r), &norms[(wave + WAVES * i) * 4][0], 0);
         }
     }
     // whether a row of the stage does not take part
@@ -962,10 +897,10 @@ __global__ __launch_bounds__(256, 2) void scan_narrow_kernel(Scan a)
 // One word from all of a wave's, by an operation that does not mind order or repetition
 template <class Of> __device__ inline u32 wave_all(u32 x, Of of)
 {
-    x = of(x, mx_from<kSwap1>(x));
-    x = of(x, mx_from<kSwap2>(x));
-    x = of(x, mx_from<kDown4>(x));
-    x = of(x, mx_from<kDown8>(x));
+    x = of(x, lane_from<kSwap1>(x));
+    x = of(x, lane_from<kSwap2>(x));
+    x = of(x, lane_from<kDown4>(x));
+    x = of(x, lane_from<kDown8>(x));
     const u32 a = __builtin_amdgcn_readlane(x, 0), b = __builtin_amdgcn_readlane(x, 16);
     const u32 c = __builtin_amdgcn_readlane(x, 32), d = __builtin_amdgcn_readlane(x, 48);
     return of(of(a, b), of(c, d));
@@ -1172,9 +1107,9 @@ __device__ inline float score_rows(const Table &t, const Table &q, ScoreLds<S> *
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const u32 row = whole ? lane_codes : __umul24(min(lane >> 2, t.n - 1 - row0[i]), t.nb) * 16;
-                mx_stage(t.codes + (size_t)row0[i] * t.nb * 16 + (row + block), &lds->codes[s * 4 + i][0], 1);
+                stage_lds(t.codes + (size_t)row0[i] * t.nb * 16 + (row + block), &lds->codes[s * 4 + i][0], 1);
             }
-            mx_stage(lane_scales + 4 * (s0 + s), &lds->scales[s][0][0], 0);
+            stage_lds(lane_scales + 4 * (s0 + s), &lds->scales[s][0][0], 0);
         }
         Operand y[S];
 #pragma unroll
@@ -1399,24 +1334,12 @@ int launch_scan_any(Scan a, hipStream_t st)
     return EFANNA_OK;
 }
 
-constexpr int64_t kMaxRows = 2147483647LL - 65536;
-
 inline bool table_ok(const uint8_t *codes, const uint8_t *scales, int64_t n, int32_t d)
 {
     if (n < 0 || n > kMaxRows || d < 1 || d > EFANNA_MX_MAX_D) return false;
     return n == 0 || (codes && scales && ((uintptr_t)codes & 15) == 0 && ((uintptr_t)scales & 3) == 0);
 }
-inline bool dtype_ok(int32_t dtype) { return dtype == EFANNA_F32 || dtype == EFANNA_F16 || dtype == EFANNA_BF16; }
-inline bool aligned_for(const void *p, int32_t dtype) { return ((uintptr_t)p & (dtype == EFANNA_F32 ? 3 : 1)) == 0; }
-
 }  // namespace
-
-#define EF_MX_DTYPE(dtype, T, ...)                                   \
-    do {                                                             \
-        if ((dtype) == EFANNA_F32) { typedef float T; __VA_ARGS__; } \
-        else if ((dtype) == EFANNA_F16) { typedef _Float16 T; __VA_ARGS__; } \
-        else { typedef __bf16 T; __VA_ARGS__; }                      \
-    } while (0)
 
 extern "C" int efanna_mx_quantise(const void *X, int32_t dtype, int64_t n, int32_t d, int64_t ldx, uint8_t *codes,
                                   uint8_t *scales, float *norms, void *stream)
@@ -1431,7 +1354,7 @@ extern "C" int efanna_mx_quantise(const void *X, int32_t dtype, int64_t n, int32
     const int64_t rows = 256 / group, slice = kSliceBlocks * rows;      // rows of a workgroup, of a launch
     for (int64_t first = 0; first < n; first += slice) {
         const int64_t here = n - first < slice ? n - first : slice;
-        EF_MX_DTYPE(dtype, T, (quantise_kernel<T><<<(unsigned)((here + rows - 1) / rows), 256, 0, st>>>(
+        EF_DTYPE(dtype, T, (quantise_kernel<T><<<(unsigned)((here + rows - 1) / rows), 256, 0, st>>>(
                                   (const T *)X + first * ldx, here, d, ldx, group, nb, sp, codes + (size_t)first * nb * 16,
                                   scales + (size_t)first * sp, norms + first)));
         EF_HIP_CHECK(hipGetLastError());
@@ -1458,7 +1381,7 @@ extern "C" int efanna_mx_rows(const uint8_t *codes, const uint8_t *scales, int64
         // (without ids the slice's rows are a table of their own)
         const Table from = ids ? t : Table{codes + (size_t)first * t.nb * 16, scales + (size_t)first * t.sp, nullptr, (int)(n - first), t.nb, t.sp};
         const int *slice_ids = ids ? ids + first : nullptr;
-        EF_MX_DTYPE(dtype, T, {
+        EF_DTYPE(dtype, T, {
             T *to = (T *)out + (size_t)first * d;
             if (past_cache) rows_kernel<T, true><<<blocks, 256, 0, st>>>(from, d, slice_ids, here, group, factor, to);
             else rows_kernel<T, false><<<blocks, 256, 0, st>>>(from, d, slice_ids, here, group, factor, to);
@@ -1480,7 +1403,7 @@ extern "C" int efanna_mx_product(const uint8_t *a_codes, const uint8_t *a_scales
     const int nb = mx_blocks(d), sp = mx_scale_pitch(d);
     const Table a = {a_codes, a_scales, nullptr, (int)m, nb, sp}, b = {b_codes, b_scales, nullptr, (int)n, nb, sp};
     int rc = EFANNA_OK;
-    EF_MX_DTYPE(dtype, T, rc = launch_product<T>(a, b, (T *)out, ldo, st));
+    EF_DTYPE(dtype, T, rc = launch_product<T>(a, b, (T *)out, ldo, st));
     if (rc != EFANNA_OK) return rc;
     EF_HIP_CHECK(hipGetLastError());
     return EFANNA_OK;
