@@ -313,37 +313,269 @@ __device__ inline bf16x8 without_infinities(bf16x8 x)
     return __builtin_bit_cast(bf16x8, u);
 }
 
-// A wave per 32 x 32 results, elements from memory one by one.
-template <class Y, class T, int FORMAT>
-__global__ __launch_bounds__(256) void f8_gradient_kernel(const Y *dy, long long ldy, long long m, int n, F8 x, int d, T *out,
-                                                          long long ldo, int tiles_d, u32 tiles)
+// Out through LDS, 32 rows of a wave's piece of 32 FA rows and 32 FB columns at a time, so that stores are whole rows of it.
+template <class T, int FA, int FB>
+__device__ inline void store_piece(const f32x16 (&acc)[FA][FB], char *lds, int lane, T *out, long long ldo, int rows, int columns)
 {
-    const int lane = threadIdx.x & 63, r = lane & 31, half = lane >> 5;
-    const u32 tile = min(blockIdx.x * 4 + (threadIdx.x >> 6), tiles - 1);
-    const int j = (int)(tile / tiles_d) * 32 + r, c0 = (int)(tile % tiles_d) * 32, c = min(c0 + r, d - 1);
-    f32x16 acc = {};
-    for (long long t0 = 0; t0 < m; t0 += 16) {
-        bf16x8 held, part[Parts<Y>::count];
+    constexpr int kAcross = 32 * FB, kPitch = kAcross + 8, kPer = 16 / sizeof(T), kLanes = kAcross / kPer;      // lanes per row
+    typedef T Out __attribute__((ext_vector_type(kPer), aligned(sizeof(T))));
+    typedef T Turn __attribute__((ext_vector_type(4), aligned(8)));
+    T *turn = (T *)lds;
+    const int r = lane & 31, half = lane >> 5;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const long long t = t0 + 8 * half + k, row = min(t, m - 1);
-            float v[4];
-            four_values<FORMAT>(x.row(row)[c], v);
-            held[k] = (__bf16)(t < m ? v[0] * scale_value(x.scales[(size_t)row * x.sp + (c >> 7)]) : 0.0f);
-            __bf16 p[Parts<Y>::count];
-            Parts<Y>::split(t < m ? dy[row * ldy + min(j, n - 1)] : (Y)0.0f, p);
+    for (int y = 0; y < FA; ++y) {
 #pragma unroll
-            for (int i = 0; i < Parts<Y>::count; ++i) part[i][k] = p[i];
+        for (int x = 0; x < FB; ++x)
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                *(Turn *)&turn[r * kPitch + 32 * x + 8 * c + 4 * half] =
+                    Turn{from_float<T>(acc[y][x][4 * c]), from_float<T>(acc[y][x][4 * c + 1]), from_float<T>(acc[y][x][4 * c + 2]),
+                         from_float<T>(acc[y][x][4 * c + 3])};
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
+        const int j = lane % kLanes * kPer, left = columns - j;
+#pragma unroll
+        for (int i = lane / kLanes; i < 32; i += 64 / kLanes) {
+            if (32 * y + i >= rows) continue;
+            T *o = out + (size_t)(32 * y + i) * ldo + j;
+            const T *from = &turn[i * kPitch + j];
+            if (left >= kPer) *(Out *)o = *(const Out *)from;
+            else
+                for (int c = 0; c < left; ++c) o[c] = from[c];
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// Which tile (row, column of tiles) and part of the sum a workgroup takes: a chiplet (every eighth workgroup) gets a connected
+// piece of them, part by part, in strips of eight rows of tiles, so that what runs there together shares operands in its L2.
+struct Place {
+    int y, x, part;
+};
+__device__ inline Place place_of(u32 id, int tiles_y, int tiles_x, int parts)
+{
+    const int tiles = tiles_y * tiles_x, all = tiles * parts, each = all / 8, more = all % 8, xcd = id & 7;
+    int at = xcd * each + min(xcd, more) + (int)(id >> 3);
+    const int part = parts > 1 ? at / tiles : 0;
+    at -= part * tiles;
+    const int strip = at / (8 * tiles_x), high = min(8, tiles_y - strip * 8), in = at - strip * 8 * tiles_x;
+    return {strip * 8 + in % high, in / high, part};
+}
+
+// WY x WX waves share a tile of dY's columns by the table's, FY x FX instructions of 32 x 32 x 16 each, and kStep rows are a
+// stage.  Both operands are wanted by columns and lie in rows: rows go to LDS as bfloat16 numbers (dY in its parts, codes with
+// their scale applied, through registers: a stage is loaded while the one before the last is multiplied) and come back through
+// transposing reads, of which a lane gets four rows' values of its column.  A row's pieces of 16 columns (32 bytes) lie in the
+// order u ^ kTurn(row), so that the eight rows that a read touches are in different banks.
+constexpr int kStep = 32;
+__device__ inline int turn_of(int row) { return 2 * (row & 3) + ((row >> 2) & 1); }
+
+template <class Y, int FY, int FX, int WY, int WX>
+struct GradientTile {
+    static constexpr int waves = WY * WX, threads = 64 * waves, across_y = 32 * FY * WY, across_x = 32 * FX * WX, parts = Parts<Y>::count;
+    static constexpr int pieces_y = across_y / 8 * kStep / threads, pieces_x = across_x / 16 * kStep / threads;      // of a thread
+    static_assert(pieces_y * threads * 8 == across_y * kStep && pieces_x * threads * 16 == across_x * kStep, "every thread loads as much");
+    struct Lds {
+        __bf16 y[2][parts][kStep][across_y], x[2][kStep][across_x];
+    };
+    static constexpr int turn_bytes = 32 * (32 * FX + 8) * 4;        // of a wave, at the end
+    static constexpr int lds = (int)sizeof(Lds) > waves * turn_bytes ? (int)sizeof(Lds) : waves * turn_bytes;
+};
+
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+
+template <class Y, int FORMAT, int FY, int FX, int WY, int WX>
+__global__ __launch_bounds__(64 * WY * WX, FY * FX > 4 ? 1 : 2) void f8_gradient_kernel(const Y *dy, long long ldy, long long m, int n, F8 x, int d,
+                                                                                       int dtype, void *out, long long ldo, int tiles_y,
+                                                                                       int tiles_x, int parts, float *partial)
+{
+    typedef GradientTile<Y, FY, FX, WY, WX> Tile;
+    typedef Y Eight __attribute__((ext_vector_type(8), aligned(sizeof(Y))));
+    extern __shared__ __align__(16) char lds_raw[];
+    typename Tile::Lds &lds = *(typename Tile::Lds *)lds_raw;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
+    const Place at = place_of(blockIdx.x, tiles_y, tiles_x, parts);
+    const int j0 = at.y * Tile::across_y, c0 = at.x * Tile::across_x;
+    const int stages = (int)((m + kStep - 1) / kStep), s_lo = (int)((long long)stages * at.part / parts),
+              s_hi = (int)((long long)stages * (at.part + 1) / parts);
+
+    Eight raw_y[Tile::pieces_y];
+    i32x4 raw_x[Tile::pieces_x];
+    u32 raw_scale[Tile::pieces_x];
+    const auto load = [&](int stage) {
+#pragma unroll
+        for (int i = 0; i < Tile::pieces_y; ++i) {
+            const int p = tid + Tile::threads * i, col = j0 + p % (Tile::across_y / 8) * 8;
+            const Y *from = dy + min((long long)stage * kStep + p / (Tile::across_y / 8), m - 1) * ldy;
+            if (col + 8 <= n) raw_y[i] = *(const Eight *)(from + col);
+            else
+#pragma unroll
+                for (int k = 0; k < 8; ++k) raw_y[i][k] = from[min(col + k, n - 1)];        // (columns past the last one are not stored)
         }
 #pragma unroll
-        for (int i = 0; i < Parts<Y>::count; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(i ? without_infinities(held) : held, part[i], acc, 0, 0, 0);
-    }
-    if (j >= n) return;
+        for (int i = 0; i < Tile::pieces_x; ++i) {
+            const int p = tid + Tile::threads * i, piece = min(c0 / 16 + p % (Tile::across_x / 16), x.nb * 8 - 1);
+            const long long row = min((long long)stage * kStep + p / (Tile::across_x / 16), m - 1);
+            raw_x[i] = *(const i32x4 *)(x.row(row) + piece * 16);
+            raw_scale[i] = x.scales[(size_t)row * x.sp + (piece >> 3)];
+        }
+    };
+    const auto put = [&](int stage) {
+        const int buffer = stage & 1;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const int col = c0 + 8 * (i >> 2) + 4 * half + (i & 3);
-        if (col < d) out[(size_t)j * ldo + col] = from_float<T>(acc[i]);
+        for (int i = 0; i < Tile::pieces_y; ++i) {
+            const int p = tid + Tile::threads * i, piece = p % (Tile::across_y / 8), row = p / (Tile::across_y / 8);
+            const bool live = (long long)stage * kStep + row < m;
+            bf16x8 part[Tile::parts];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                __bf16 one[Tile::parts];
+                Parts<Y>::split(live ? raw_y[i][k] : (Y)0.0f, one);
+#pragma unroll
+                for (int q = 0; q < Tile::parts; ++q) part[q][k] = one[q];
+            }
+#pragma unroll
+            for (int q = 0; q < Tile::parts; ++q)
+                *(bf16x8 *)&lds.y[buffer][q][row][((piece >> 1) ^ turn_of(row)) * 16 + (piece & 1) * 8] = part[q];
+        }
+#pragma unroll
+        for (int i = 0; i < Tile::pieces_x; ++i) {
+            const int p = tid + Tile::threads * i, piece = p % (Tile::across_x / 16), row = p / (Tile::across_x / 16);
+            const bool live = (long long)stage * kStep + row < m;
+            bf16x8 wide[2];
+            sixteen_wide<FORMAT>(live ? raw_x[i] : i32x4{0, 0, 0, 0}, scale_value(live ? raw_scale[i] : 127), wide);
+            __bf16 *to = &lds.x[buffer][row][(piece ^ turn_of(row)) * 16];
+            *(bf16x8 *)to = wide[0];
+            *(bf16x8 *)(to + 8) = wide[1];
+        }
+    };
+
+    f32x16 acc[FY][FX] = {};
+    const int wy = wave % WY, wx = wave / WY;
+    // a lane's part of a transposing read: row 4 half + (lane / 4) % 4 of eight, a quarter of the piece of its 16 lanes
+    const int row = 4 * half + ((lane >> 2) & 3), group = (lane >> 4) & 1, quarter = (lane & 3) * 4;
+    int at_y[FY], at_x[FX];
+#pragma unroll
+    for (int f = 0; f < FY; ++f) at_y[f] = row * Tile::across_y + (((wy * FY + f) * 2 + group) ^ turn_of(row)) * 16 + quarter;
+#pragma unroll
+    for (int f = 0; f < FX; ++f) at_x[f] = row * Tile::across_x + (((wx * FX + f) * 2 + group) ^ turn_of(row)) * 16 + quarter;
+    const auto columns = [](const __bf16 *first, int pitch) {      // sixteen rows' values of the lane's column, as an operand
+        const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)first);
+        const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(first + 8 * pitch));
+        typedef short i16x8 __attribute__((ext_vector_type(8)));
+        return __builtin_bit_cast(bf16x8, (i16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    const auto multiply = [&](int stage) {
+        const int buffer = stage & 1;
+#pragma unroll
+        for (int k = 0; k < kStep; k += 16) {
+            bf16x8 fx[FX], fx_finite[FX];
+#pragma unroll
+            for (int f = 0; f < FX; ++f) {
+                fx[f] = columns(&lds.x[buffer][k][0] + at_x[f], Tile::across_x);
+                if (Tile::parts > 1) fx_finite[f] = without_infinities(fx[f]);
+            }
+#pragma unroll
+            for (int q = 0; q < Tile::parts; ++q) {
+                bf16x8 fy[FY];
+#pragma unroll
+                for (int f = 0; f < FY; ++f) fy[f] = columns(&lds.y[buffer][q][k][0] + at_y[f], Tile::across_y);
+#pragma unroll
+                for (int a = 0; a < FY; ++a)
+#pragma unroll
+                    for (int b = 0; b < FX; ++b)
+                        acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q ? fx_finite[b] : fx[b], fy[a], acc[a][b], 0, 0, 0);
+            }
+        }
+    };
+    const auto meet = [&]() {          // what was written to LDS is there, what was read has arrived
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    if (s_lo < s_hi) {
+        load(s_lo);
+        put(s_lo);
+        if (s_lo + 1 < s_hi) load(s_lo + 1);
+        meet();
+        for (int stage = s_lo; stage < s_hi; ++stage) {
+            if (stage + 1 < s_hi) put(stage + 1);
+            if (stage + 2 < s_hi) load(stage + 2);
+            multiply(stage);
+            meet();
+        }
     }
+    const int rows = n - j0 - wy * FY * 32, cols = d - c0 - wx * FX * 32;
+    const size_t first_row = j0 + wy * FY * 32, first_col = c0 + wx * FX * 32;
+    char *turn = lds_raw + wave * Tile::turn_bytes;
+    if (parts > 1) store_piece<float>(acc, turn, lane, partial + ((size_t)at.part * n + first_row) * d + first_col, d, rows, cols);
+    else
+        EF_DTYPE(dtype, T, store_piece<T>(acc, turn, lane, (T *)out + first_row * ldo + first_col, ldo, rows, cols));
+}
+
+// Sums of the parts, in their order.
+template <class T>
+__global__ __launch_bounds__(256) void f8_join_kernel(const float *partial, int parts, u32 rows, u32 columns, T *out, long long ldo)
+{
+    const u32 row = blockIdx.y, c = (blockIdx.x * 256 + threadIdx.x) * 4;
+    if (c >= columns) return;
+    typedef float Four __attribute__((ext_vector_type(4), aligned(4)));
+    const size_t step = (size_t)rows * columns;
+    const float *from = partial + (size_t)row * columns + c;
+    f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (c + 4 <= columns) {
+        for (int p = 0; p < parts; ++p) sum += (f32x4) * (const Four *)(from + p * step);
+        T *o = out + (size_t)row * ldo + c;
+        typedef T Out __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+        *(Out *)o = Out{from_float<T>(sum[0]), from_float<T>(sum[1]), from_float<T>(sum[2]), from_float<T>(sum[3])};
+    } else
+        for (u32 i = c; i < columns; ++i) {
+            float one = 0.0f;
+            for (int p = 0; p < parts; ++p) one += from[p * step + i - c];
+            out[(size_t)row * ldo + i] = from_float<T>(one);
+        }
+}
+
+template <class T>
+int launch_join(const float *partial, int parts, int64_t rows, int64_t columns, T *out, int64_t ldo, hipStream_t st)
+{
+    const dim3 grid((unsigned)((columns + 1023) / 1024), (unsigned)rows);
+    f8_join_kernel<T><<<grid, 256, 0, st>>>(partial, parts, (u32)rows, (u32)columns, out, ldo);
+    EF_HIP_CHECK(hipGetLastError());
+    return EFANNA_OK;
+}
+
+// Tiles of 128 or 256 a side, and as many parts of the sum as fill the GPU.
+struct GradientShape {
+    int side, parts;
+    size_t bytes;
+};
+inline GradientShape gradient_shape(int64_t m, int32_t n, int32_t d)
+{
+    const auto tiles = [&](int side) { return (int64_t)((n + side - 1) / side) * ((d + side - 1) / side); };
+    GradientShape s;
+    s.side = tiles(256) >= 192 ? 256 : 128;
+    const int64_t room = s.side == 256 ? 256 : 512, stages = (m + kStep - 1) / kStep;
+    int64_t parts = room / tiles(s.side);
+    if (parts > stages / 8) parts = stages / 8;
+    s.parts = parts < 1 ? 1 : (int)parts;
+    s.bytes = s.parts > 1 ? align_up((size_t)s.parts * n * d * sizeof(float)) : 0;
+    return s;
+}
+
+template <class Y, int FORMAT, int FY, int FX, int WY, int WX>
+int launch_gradient(const Y *dy, int64_t ldy, int64_t m, int n, const F8 &x, int d, int dtype, void *out, int64_t ldo, int parts,
+                    float *partial, hipStream_t st)
+{
+    typedef GradientTile<Y, FY, FX, WY, WX> Tile;
+    const int ty = (n + Tile::across_y - 1) / Tile::across_y, tx = (d + Tile::across_x - 1) / Tile::across_x;
+    EF_HIP_CHECK(allow_lds((const void *)f8_gradient_kernel<Y, FORMAT, FY, FX, WY, WX>, Tile::lds));
+    f8_gradient_kernel<Y, FORMAT, FY, FX, WY, WX><<<(unsigned)(ty * tx * parts), Tile::threads, Tile::lds, st>>>(
+        dy, ldy, m, n, x, d, dtype, out, ldo, ty, tx, parts, partial);
+    EF_HIP_CHECK(hipGetLastError());
+    return EFANNA_OK;
 }
 
 inline bool table_ok(const uint8_t *codes, const uint8_t *scales, int32_t format, int64_t n, int32_t d)
@@ -447,7 +679,11 @@ extern "C" int efanna_f8_product(const uint8_t *a_codes, const uint8_t *a_scales
     return EFANNA_OK;
 }
 
-extern "C" size_t efanna_f8_gradient_workspace_bytes(int64_t m, int32_t n, int32_t d) { return 0; }
+extern "C" size_t efanna_f8_gradient_workspace_bytes(int64_t m, int32_t n, int32_t d)
+{
+    if (m < 0 || m > kMaxRows || n < 1 || n > EFANNA_F8_MAX_D || d < 1 || d > EFANNA_F8_MAX_D) return 0;
+    return gradient_shape(m, n, d).bytes;
+}
 
 extern "C" int efanna_f8_gradient(const void *dY, int32_t dtype, int64_t m, int32_t n, int64_t ldy, const uint8_t *codes,
                                   const uint8_t *scales, int32_t format, int32_t d, int32_t out_dtype, void *out,
@@ -457,12 +693,16 @@ extern "C" int efanna_f8_gradient(const void *dY, int32_t dtype, int64_t m, int3
         return EFANNA_EINVAL;
     if (n == 0) return EFANNA_OK;
     if ((m > 0 && !dY) || !out || !aligned_for(dY, dtype) || !aligned_for(out, out_dtype)) return EFANNA_EINVAL;
-    if (!workspace_ok(ws, ws_bytes, efanna_f8_gradient_workspace_bytes(m, n, d))) return EFANNA_EWORKSPACE;
+    const GradientShape sh = gradient_shape(m, n, d);
+    if (!workspace_ok(ws, ws_bytes, sh.bytes)) return EFANNA_EWORKSPACE;
+    hipStream_t st = (hipStream_t)stream;
     const F8 x = {codes, scales, (int)m, f8_blocks(d), f8_scale_pitch(d)};
-    const int tiles_d = (d + 31) / 32;
-    const u32 tiles = (u32)((n + 31) / 32) * (u32)tiles_d;
-    EF_DTYPE(dtype, Y, EF_DTYPE(out_dtype, T, EF_FORMAT(format, F, (f8_gradient_kernel<Y, T, F><<<(tiles + 3) / 4, 256, 0, (hipStream_t)stream>>>(
-                           (const Y *)dY, ldy, m, n, x, d, (T *)out, ldo, tiles_d, tiles)))));
-    EF_HIP_CHECK(hipGetLastError());
-    return EFANNA_OK;
+    int rc = EFANNA_OK;
+    EF_DTYPE(dtype, Y, EF_FORMAT(format, F, {
+        if (sh.side == 256) rc = launch_gradient<Y, F, 4, 2, 2, 4>((const Y *)dY, ldy, m, n, x, d, out_dtype, out, ldo, sh.parts, (float *)ws, st);
+        else rc = launch_gradient<Y, F, 2, 2, 2, 2>((const Y *)dY, ldy, m, n, x, d, out_dtype, out, ldo, sh.parts, (float *)ws, st);
+    }));
+    if (rc != EFANNA_OK || sh.parts == 1) return rc;
+    EF_DTYPE(out_dtype, T, rc = launch_join<T>((const float *)ws, sh.parts, n, d, (T *)out, ldo, st));
+    return rc;
 }
