@@ -7,6 +7,8 @@
 
 #include "../../include/efanna_f8.h"
 
+#include <type_traits>
+
 namespace {
 
 __host__ __device__ inline int f8_blocks(int d) { return (d + 127) >> 7; }
@@ -240,79 +242,6 @@ template <int FA, int FB> __device__ inline f32x16 f8_mma(i32x4 a0, i32x4 a1, in
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, FA, FB, 0, a_scale, 0, b_scale);
 }
 
-// Products: a wave per 32 x 32 results, operands from memory.
-template <class T, int FA, int FB>
-__global__ __launch_bounds__(256) void f8_product_kernel(F8 a, F8 b, T *out, long long ldo, int tiles_b, u32 tiles)
-{
-    const int lane = threadIdx.x & 63, r = lane & 31, half = lane >> 5;
-    const u32 tile = min(blockIdx.x * 4 + (threadIdx.x >> 6), tiles - 1);
-    const int i0 = (int)(tile / tiles_b) * 32, j0 = (int)(tile % tiles_b) * 32;
-    const int ra = min(i0 + r, a.n - 1), rb = min(j0 + r, b.n - 1);
-    f32x16 acc = {};
-    for (int s = 0; s < a.nb; ++s) {
-        const int sa = a.scales[(size_t)ra * a.sp + s], sb = b.scales[(size_t)rb * b.sp + s];
-        const i32x4 *pa = (const i32x4 *)(a.row(ra) + s * 128) + half, *pb = (const i32x4 *)(b.row(rb) + s * 128) + half;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            if constexpr (sizeof(T) == 4) {
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    bf16x8 x[2], y[2];
-                    sixteen_wide<FB>(pb[4 * h + 2 * c], scale_value(sb), x);
-                    sixteen_wide<FA>(pa[4 * h + 2 * c], scale_value(sa), y);
-                    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[0], y[0], acc, 0, 0, 0);
-                    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[1], y[1], acc, 0, 0, 0);
-                }
-            } else
-                acc = f8_mma<FB, FA>(pb[4 * h], pb[4 * h + 2], sb, pa[4 * h], pa[4 * h + 2], sa, acc);
-        }
-    }
-    if (i0 + r >= a.n) return;
-#pragma unroll
-    for (int c = 0; c < 16; ++c) {
-        const int j = j0 + 8 * (c >> 2) + 4 * half + (c & 3);
-        if (j < b.n) out[(size_t)(i0 + r) * ldo + j] = from_float<T>(acc[c]);
-    }
-}
-
-// ---- gradient of the weights -----------------------------------------------------------------------------
-// A number as a sum of bfloat16 numbers, exactly (from 2^-110 on for float32): one of its own kind, two of half precision (11
-// bits), three of float32 (24 bits).  Infinities and NaN are all in the first part.
-template <class Y> struct Parts;
-template <> struct Parts<__bf16> {
-    static constexpr int count = 1;
-    static __device__ inline void split(__bf16 x, __bf16 (&p)[1]) { p[0] = x; }
-};
-template <> struct Parts<_Float16> {
-    static constexpr int count = 2;
-    static __device__ inline void split(_Float16 h, __bf16 (&p)[2])
-    {
-        const float x = (float)h;
-        p[0] = (__bf16)x;
-        p[1] = (__bf16)(finite_bits(x) ? x - (float)p[0] : 0.0f);
-    }
-};
-template <> struct Parts<float> {
-    static constexpr int count = 3;
-    static __device__ inline float cut(float x) { return __uint_as_float(__float_as_uint(x) & 0xFFFF0000u); }
-    static __device__ inline void split(float x, __bf16 (&p)[3])
-    {
-        const bool finite = finite_bits(x) != 0;
-        const float first = finite ? cut(x) : x, rest = finite ? x - first : 0.0f, second = cut(rest);
-        p[0] = (__bf16)first, p[1] = (__bf16)second, p[2] = (__bf16)(rest - second);
-    }
-};
-
-// What the parts after the first are multiplied by: numbers without the infinities, which the first part meets (a later
-// part that is zero would make a NaN of one).
-typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
-__device__ inline bf16x8 without_infinities(bf16x8 x)
-{
-    u16x8 u = __builtin_bit_cast(u16x8, x);
-    u *= __builtin_elementwise_min((u16x8)((u & (unsigned short)0x7FFF) ^ (unsigned short)0x7F80), (u16x8)(unsigned short)1);
-    return __builtin_bit_cast(bf16x8, u);
-}
-
 // Out through LDS, 32 rows of a wave's piece of 32 FA rows and 32 FB columns at a time, so that stores are whole rows of it.
 template <class T, int FA, int FB>
 __device__ inline void store_piece(const f32x16 (&acc)[FA][FB], char *lds, int lane, T *out, long long ldo, int rows, int columns)
@@ -361,6 +290,391 @@ __device__ inline Place place_of(u32 id, int tiles_y, int tiles_x, int parts)
     at -= part * tiles;
     const int strip = at / (8 * tiles_x), high = min(8, tiles_y - strip * 8), in = at - strip * 8 * tiles_x;
     return {strip * 8 + in % high, in / high, part};
+}
+
+// Sums of the parts, in their order.
+template <class T>
+__global__ __launch_bounds__(256) void f8_join_kernel(const float *partial, int parts, u32 rows, u32 columns, T *out, long long ldo)
+{
+    const u32 row = blockIdx.y, c = (blockIdx.x * 256 + threadIdx.x) * 4;
+    if (c >= columns) return;
+    typedef float Four __attribute__((ext_vector_type(4), aligned(4)));
+    const size_t step = (size_t)rows * columns;
+    const float *from = partial + (size_t)row * columns + c;
+    f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (c + 4 <= columns) {
+        for (int p = 0; p < parts; ++p) sum += (f32x4) * (const Four *)(from + p * step);
+        T *o = out + (size_t)row * ldo + c;
+        typedef T Out __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+        *(Out *)o = Out{from_float<T>(sum[0]), from_float<T>(sum[1]), from_float<T>(sum[2]), from_float<T>(sum[3])};
+    } else
+        for (u32 i = c; i < columns; ++i) {
+            float one = 0.0f;
+            for (int p = 0; p < parts; ++p) one += from[p * step + i - c];
+            out[(size_t)row * ldo + i] = from_float<T>(one);
+        }
+}
+
+template <class T>
+int launch_join(const float *partial, int parts, int64_t rows, int64_t columns, T *out, int64_t ldo, hipStream_t st)
+{
+    const dim3 grid((unsigned)((columns + 1023) / 1024), (unsigned)rows);
+    f8_join_kernel<T><<<grid, 256, 0, st>>>(partial, parts, (u32)rows, (u32)columns, out, ldo);
+    EF_HIP_CHECK(hipGetLastError());
+    return EFANNA_OK;
+}
+
+// ---- products --------------------------------------------------------------------------------------------
+// out[i][j] = a_i . b_j.  The rows of b are the instruction's rows and those of a its columns, so that a lane ends up with
+// consecutive values of an output row.
+
+// WA x WB waves share a tile of a's rows by b's rows, FA x FB instructions of 32 x 32 each.  A stage is a block of both, whole
+// lines of 128 bytes, and every fourth one brings the scales of four; while one is computed the next is on its way into LDS.  A
+// load of codes brings 8 rows; the 16-byte pieces of row r lie in the order p ^ (r / 2) % 8, so that pieces p of 16 rows,
+// which are read together, are in different ones of the 64 banks.  WIDE: codes are turned into bfloat16 numbers on their way from
+// LDS, scales applied, so that products and sums are those of float32.
+template <int FA, int FB, int WA, int WB>
+struct ProductTile {
+    static constexpr int waves = WA * WB, side_a = 32 * FA * WA, side_b = 32 * FB * WB, sides = side_a + side_b;
+    static constexpr int each = sides / 8 / waves, each_scales = sides / 64 / waves;      // loads of a wave
+    static_assert(each_scales * 64 * waves == sides, "every wave loads as much");
+    struct Lds {
+        u32 codes[2][sides / 8][256];       // a's rows, then b's
+        u32 scales[2][sides];               // of four blocks
+    };
+    static constexpr int turn_bytes = 32 * (32 * FB + 8) * 4;        // of a wave, at the end
+    static constexpr int lds = (int)sizeof(Lds) > waves * turn_bytes ? (int)sizeof(Lds) : waves * turn_bytes;
+};
+
+template <bool WIDE, int FORMAT_A, int FORMAT_B, int FA, int FB, int WA, int WB>
+__global__ __launch_bounds__(64 * WA * WB, FA * FB > 4 ? 1 : 2) void f8_product_tile_kernel(F8 a, F8 b, int dtype, void *out, long long ldo,
+                                                                                           int tiles_a, int tiles_b, int parts, float *partial)
+{
+    typedef ProductTile<FA, FB, WA, WB> Tile;
+    extern __shared__ __align__(16) char lds_raw[];
+    typename Tile::Lds &lds = *(typename Tile::Lds *)lds_raw;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 31, half = lane >> 5;
+    const Place at = place_of(blockIdx.x, tiles_a, tiles_b, parts);
+    const int i0 = at.y * Tile::side_a, j0 = at.x * Tile::side_b;
+    const int rows_a = a.n - i0, rows_b = b.n - j0;
+    // a part is whole groups of four blocks
+    const int fours = (a.nb + 3) / 4, s_lo = (int)((long long)fours * at.part / parts) * 4,
+              s_hi = min((int)((long long)fours * (at.part + 1) / parts) * 4, a.nb);
+    const uint8_t *codes_a = a.row(i0), *codes_b = b.row(j0), *scales_a = a.scales + (size_t)i0 * a.sp, *scales_b = b.scales + (size_t)j0 * b.sp;
+    const auto row_of = [&](int row) { return (u32)(row < Tile::side_a ? min(row, rows_a - 1) : min(row - Tile::side_a, rows_b - 1)); };
+    u32 at_codes[Tile::each], at_scales[Tile::each_scales];
+#pragma unroll
+    for (int i = 0; i < Tile::each; ++i) {
+        const int row = (wave * Tile::each + i) * 8 + (lane >> 3);
+        at_codes[i] = row_of(row) * a.nb * 128 + ((lane & 7) ^ ((row >> 1) & 7)) * 16;
+    }
+#pragma unroll
+    for (int i = 0; i < Tile::each_scales; ++i) at_scales[i] = row_of((wave * Tile::each_scales + i) * 64 + lane) * a.sp;
+    const auto load = [&](int stage, bool with_scales) {
+#pragma unroll
+        for (int i = 0; i < Tile::each; ++i) {
+            const int op = wave * Tile::each + i;
+            stage_lds((op * 8 < Tile::side_a ? codes_a : codes_b) + stage * 128 + at_codes[i], &lds.codes[stage & 1][op][0], 1);
+        }
+        if (!with_scales) return;
+#pragma unroll
+        for (int i = 0; i < Tile::each_scales; ++i) {
+            const int op = wave * Tile::each_scales + i;
+            stage_lds((op * 64 < Tile::side_a ? scales_a : scales_b) + stage + at_scales[i], &lds.scales[(stage >> 2) & 1][op * 64], 0);
+        }
+    };
+    f32x16 acc[FA][FB] = {};
+    const int wa = wave % WA * 32 * FA, wb = wave / WA * 32 * FB;
+    // where the lane's first piece is in a stage (other pieces: the offset ^ 16 p; 32 rows further down: 4096 bytes on)
+    const int code_a = (wa + r) * 128 + (half ^ ((r >> 1) & 7)) * 16, code_b = code_a + (Tile::side_a + wb - wa) * 128;
+    const auto piece = [&](int stage, int from, int p) { return *(const i32x4 *)((const char *)lds.codes[stage & 1] + (from ^ (16 * p))); };
+    int sa[FA], sb[FB];
+    const auto read_scales = [&](int stage) {
+        const u32 *from = &lds.scales[(stage >> 2) & 1][r];
+        const int shift = 8 * (stage & 3);
+#pragma unroll
+        for (int f = 0; f < FA; ++f) sa[f] = (int)(from[wa + 32 * f] >> shift);
+#pragma unroll
+        for (int f = 0; f < FB; ++f) sb[f] = (int)(from[Tile::side_a + wb + 32 * f] >> shift);
+    };
+    const auto multiply = [&](int stage) {
+        read_scales(stage);
+        if constexpr (WIDE) {
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+                bf16x8 wide_b[FB][2];
+#pragma unroll
+                for (int f = 0; f < FB; ++f) sixteen_wide<FORMAT_B>(piece(stage, code_b + 4096 * f, 2 * p), scale_value(sb[f] & 255), wide_b[f]);
+#pragma unroll
+                for (int y = 0; y < FA; ++y) {
+                    bf16x8 wide_a[2];
+                    sixteen_wide<FORMAT_A>(piece(stage, code_a + 4096 * y, 2 * p), scale_value(sa[y] & 255), wide_a);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int x = 0; x < FB; ++x) acc[y][x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wide_b[x][h], wide_a[h], acc[y][x], 0, 0, 0);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                i32x4 cb[FB][2], ca[FA][2];
+#pragma unroll
+                for (int f = 0; f < FB; ++f)
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) cb[f][q] = piece(stage, code_b + 4096 * f, 4 * h + 2 * q);
+#pragma unroll
+                for (int f = 0; f < FA; ++f)
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) ca[f][q] = piece(stage, code_a + 4096 * f, 4 * h + 2 * q);
+#pragma unroll
+                for (int y = 0; y < FA; ++y)
+#pragma unroll
+                    for (int x = 0; x < FB; ++x)
+                        acc[y][x] = f8_mma<FORMAT_B, FORMAT_A>(cb[x][0], cb[x][1], sb[x], ca[y][0], ca[y][1], sa[y], acc[y][x]);
+            }
+        }
+    };
+    // a stage has arrived, and what was read of the one before it is in registers
+    const auto arrived = [&]() {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    if (s_lo < s_hi) {
+        load(s_lo, true);
+        for (int stage = s_lo; stage < s_hi; ++stage) {
+            arrived();
+            if (stage + 1 < s_hi) load(stage + 1, ((stage + 1) & 3) == 0);
+            multiply(stage);
+        }
+        arrived();
+    }
+    const size_t first_row = i0 + wa, first_col = j0 + wb;
+    char *turn = lds_raw + wave * Tile::turn_bytes;
+    if (parts > 1) store_piece<float>(acc, turn, lane, partial + ((size_t)at.part * a.n + first_row) * b.n + first_col, b.n, rows_a - wa, rows_b - wb);
+    else if constexpr (WIDE) store_piece<float>(acc, turn, lane, (float *)out + first_row * ldo + first_col, ldo, rows_a - wa, rows_b - wb);
+    else if (dtype == EFANNA_F16) store_piece<_Float16>(acc, turn, lane, (_Float16 *)out + first_row * ldo + first_col, ldo, rows_a - wa, rows_b - wb);
+    else store_piece<__bf16>(acc, turn, lane, (__bf16 *)out + first_row * ldo + first_col, ldo, rows_a - wa, rows_b - wb);
+}
+
+// Few rows of a (16 M at most): bound by reading b once.  A workgroup takes 16 ROWS rows of b; its waves share the blocks, and
+// their sums meet in LDS, in the waves' order.  b's codes pass through LDS by direct loads, S blocks at a time (a load brings 8
+// whole lines, ordered as in the tiles); operands are of 16 rows, lane l brings row l % 16 and the pieces l / 16 and l / 16 + 4.
+template <int ROWS, int S>
+struct FewLds {
+    u32 codes[S][2 * ROWS][256];
+};
+template <bool WIDE, int FORMAT_A, int FORMAT_B, int M, int ROWS, int S, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void f8_product_few_kernel(F8 a, F8 b, int dtype, void *out, long long ldo)
+{
+    extern __shared__ __align__(16) char lds_raw[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
+    FewLds<ROWS, S> *lds = (FewLds<ROWS, S> *)lds_raw + wave;
+    const int j0 = blockIdx.x * 16 * ROWS, left = b.n - j0;
+    const int s_lo = a.nb * wave / WAVES, s_hi = a.nb * (wave + 1) / WAVES;
+    const uint8_t *codes_b = b.row(j0);
+    u32 at_codes[2 * ROWS];
+#pragma unroll
+    for (int i = 0; i < 2 * ROWS; ++i) {
+        const int row = 8 * i + (lane >> 3);
+        at_codes[i] = (u32)min(row, left - 1) * b.nb * 128 + ((lane & 7) ^ ((row >> 1) & 7)) * 16;
+    }
+    const uint8_t *row_a[M], *scale_a[M], *scale_b[ROWS];
+#pragma unroll
+    for (int f = 0; f < M; ++f) {
+        const int row = min(16 * f + r, a.n - 1);
+        row_a[f] = a.row(row) + g * 16, scale_a[f] = a.scales + (size_t)row * a.sp;
+    }
+#pragma unroll
+    for (int f = 0; f < ROWS; ++f) scale_b[f] = b.scales + (size_t)(j0 + min(16 * f + r, left - 1)) * b.sp;
+    f32x4 acc[M][ROWS] = {};
+    for (int s0 = s_lo; s0 < s_hi; s0 += S) {
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            if (S > 1 && s0 + s >= s_hi) break;
+#pragma unroll
+            for (int i = 0; i < 2 * ROWS; ++i) stage_lds(codes_b + (s0 + s) * 128 + at_codes[i], &lds->codes[s][i][0], 1);
+        }
+        i32x4 y[S][M][2];
+        int sy[S][M], sx[S][ROWS];
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            const int at = min(s0 + s, s_hi - 1);
+#pragma unroll
+            for (int f = 0; f < M; ++f) {
+                y[s][f][0] = *(const i32x4 *)(row_a[f] + at * 128), y[s][f][1] = *(const i32x4 *)(row_a[f] + at * 128 + 64);
+                sy[s][f] = scale_a[f][at];
+            }
+#pragma unroll
+            for (int f = 0; f < ROWS; ++f) sx[s][f] = scale_b[f][at];
+        }
+        wait_loads<0>();
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            if (S > 1 && s0 + s >= s_hi) break;
+#pragma unroll
+            for (int t = 0; t < ROWS; ++t) {
+                const char *from = (const char *)&lds->codes[s][2 * t][0] + r * 128;
+                const i32x4 x0 = *(const i32x4 *)(from + ((g ^ ((r >> 1) & 7)) * 16)), x1 = *(const i32x4 *)(from + (((g + 4) ^ ((r >> 1) & 7)) * 16));
+                if constexpr (WIDE) {
+                    bf16x8 wide_b[2][2];
+                    sixteen_wide<FORMAT_B>(x0, scale_value(sx[s][t]), wide_b[0]);
+                    sixteen_wide<FORMAT_B>(x1, scale_value(sx[s][t]), wide_b[1]);
+#pragma unroll
+                    for (int f = 0; f < M; ++f)
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) {
+                            bf16x8 wide_a[2];
+                            sixteen_wide<FORMAT_A>(y[s][f][q], scale_value(sy[s][f]), wide_a);
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) acc[f][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide_b[q][h], wide_a[h], acc[f][t], 0, 0, 0);
+                        }
+                } else {
+                    const i32x8 x = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
+#pragma unroll
+                    for (int f = 0; f < M; ++f) {
+                        const i32x4 y0 = y[s][f][0], y1 = y[s][f][1];
+                        const i32x8 ya = {y0.x, y0.y, y0.z, y0.w, y1.x, y1.y, y1.z, y1.w};
+                        acc[f][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, ya, acc[f][t], FORMAT_B, FORMAT_A, 0, sx[s][t], 0, sy[s][f]);
+                    }
+                }
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // (read before it is written again)
+    }
+    if (WAVES > 1) {
+        f32x4 *share = (f32x4 *)lds_raw;          // [wave - 1][M * ROWS][lane]
+        __syncthreads();
+        if (wave > 0)
+#pragma unroll
+            for (int f = 0; f < M; ++f)
+#pragma unroll
+                for (int t = 0; t < ROWS; ++t) share[((wave - 1) * M * ROWS + f * ROWS + t) * 64 + lane] = acc[f][t];
+        __syncthreads();
+        if (wave > 0) return;
+        for (int w = 0; w < WAVES - 1; ++w)
+#pragma unroll
+            for (int f = 0; f < M; ++f)
+#pragma unroll
+                for (int t = 0; t < ROWS; ++t) acc[f][t] += share[(w * M * ROWS + f * ROWS + t) * 64 + lane];
+    }
+    const auto store = [&](auto *to) {
+        typedef typename std::remove_reference<decltype(*to)>::type T;
+        typedef T Four __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+#pragma unroll
+        for (int f = 0; f < M; ++f)
+#pragma unroll
+            for (int t = 0; t < ROWS; ++t) {
+                const int i = 16 * f + r, j = 16 * t + 4 * g;
+                const f32x4 v = acc[f][t];
+                if (i >= a.n || j >= left) continue;
+                T *o = to + (size_t)i * ldo + j0 + j;
+                if (left - j >= 4) *(Four *)o = Four{from_float<T>(v[0]), from_float<T>(v[1]), from_float<T>(v[2]), from_float<T>(v[3])};
+                else
+                    for (int c = 0; c < left - j; ++c) o[c] = from_float<T>(v[c]);
+            }
+    };
+    if constexpr (WIDE) store((float *)out);
+    else if (dtype == EFANNA_F16) store((_Float16 *)out);
+    else store((__bf16 *)out);
+}
+
+// How a product is cut: few rows of a, or tiles of 128 or 256 a side in as many parts of the sum as fill the GPU.
+struct ProductShape {
+    bool few;
+    int side, parts;
+    size_t bytes;
+};
+constexpr int kFew = 32;
+inline ProductShape product_shape(int64_t m, int64_t n, int32_t d)
+{
+    ProductShape s = {m <= kFew, 128, 1, 0};
+    if (s.few) return s;
+    const auto tiles = [&](int64_t side) { return ((m + side - 1) / side) * ((n + side - 1) / side); };
+    if (tiles(128) > 512) s.side = 256;
+    const int64_t fours = (f8_blocks(d) + 3) / 4;
+    int64_t parts = s.side == 128 ? 512 / tiles(128) : 1;
+    if (parts > fours / 2) parts = fours / 2;
+    s.parts = parts < 1 ? 1 : (int)parts;
+    s.bytes = s.parts > 1 ? align_up((size_t)s.parts * m * n * sizeof(float)) : 0;
+    return s;
+}
+template <bool WIDE, int FORMAT_A, int FORMAT_B, int FA, int FB, int WA, int WB>
+int launch_tiles(const F8 &a, const F8 &b, int dtype, void *out, int64_t ldo, int parts, float *partial, hipStream_t st)
+{
+    typedef ProductTile<FA, FB, WA, WB> Tile;
+    const int64_t ta = ((int64_t)a.n + Tile::side_a - 1) / Tile::side_a, tb = ((int64_t)b.n + Tile::side_b - 1) / Tile::side_b;
+    if (ta * tb * parts > 2147483647LL || !launch_fits(ta * tb * parts, Tile::waves * 64)) return EFANNA_EUNSUPPORTED;
+    EF_HIP_CHECK(allow_lds((const void *)f8_product_tile_kernel<WIDE, FORMAT_A, FORMAT_B, FA, FB, WA, WB>, Tile::lds));
+    f8_product_tile_kernel<WIDE, FORMAT_A, FORMAT_B, FA, FB, WA, WB><<<(unsigned)(ta * tb * parts), Tile::waves * 64, Tile::lds, st>>>(
+        a, b, dtype, out, ldo, (int)ta, (int)tb, parts, partial);
+    EF_HIP_CHECK(hipGetLastError());
+    return EFANNA_OK;
+}
+template <bool WIDE, int FORMAT_A, int FORMAT_B, int M, int ROWS, int S, int WAVES>
+int launch_few(const F8 &a, const F8 &b, int dtype, void *out, int64_t ldo, hipStream_t st)
+{
+    const int stage = WAVES * (int)sizeof(FewLds<ROWS, S>), join = (WAVES - 1) * M * ROWS * 64 * 16, lds = stage > join ? stage : join;
+    const int64_t blocks = ((int64_t)b.n + 16 * ROWS - 1) / (16 * ROWS);
+    if (!launch_fits(blocks, 64 * WAVES)) return EFANNA_EUNSUPPORTED;
+    EF_HIP_CHECK(allow_lds((const void *)f8_product_few_kernel<WIDE, FORMAT_A, FORMAT_B, M, ROWS, S, WAVES>, lds));
+    f8_product_few_kernel<WIDE, FORMAT_A, FORMAT_B, M, ROWS, S, WAVES><<<(unsigned)blocks, 64 * WAVES, lds, st>>>(a, b, dtype, out, ldo);
+    EF_HIP_CHECK(hipGetLastError());
+    return EFANNA_OK;
+}
+template <bool WIDE, int FORMAT_A, int FORMAT_B, int M>
+int launch_few_of(const F8 &a, const F8 &b, int dtype, void *out, int64_t ldo, hipStream_t st)
+{
+    if (a.nb < 4) return launch_few<WIDE, FORMAT_A, FORMAT_B, M, 4, 1, 1>(a, b, dtype, out, ldo, st);
+    if (a.nb < 16) return launch_few<WIDE, FORMAT_A, FORMAT_B, M, 1, 1, 4>(a, b, dtype, out, ldo, st);
+    return launch_few<WIDE, FORMAT_A, FORMAT_B, M, 1, 2, 8>(a, b, dtype, out, ldo, st);
+}
+template <bool WIDE, int FORMAT_A, int FORMAT_B>
+int launch_product(const F8 &a, const F8 &b, int dtype, void *out, int64_t ldo, const ProductShape &sh, float *partial, hipStream_t st)
+{
+    if (sh.few) return a.n <= 16 ? launch_few_of<WIDE, FORMAT_A, FORMAT_B, 1>(a, b, dtype, out, ldo, st)
+                                 : launch_few_of<WIDE, FORMAT_A, FORMAT_B, 2>(a, b, dtype, out, ldo, st);
+    return sh.side == 256 ? launch_tiles<WIDE, FORMAT_A, FORMAT_B, 4, 2, 2, 4>(a, b, dtype, out, ldo, sh.parts, partial, st)
+                          : launch_tiles<WIDE, FORMAT_A, FORMAT_B, 2, 2, 2, 2>(a, b, dtype, out, ldo, sh.parts, partial, st);
+}
+
+// ---- gradient of the weights -----------------------------------------------------------------------------
+// A number as a sum of bfloat16 numbers, exactly (from 2^-110 on for float32): one of its own kind, two of half precision (11
+// bits), three of float32 (24 bits).  Infinities and NaN are all in the first part.
+template <class Y> struct Parts;
+template <> struct Parts<__bf16> {
+    static constexpr int count = 1;
+    static __device__ inline void split(__bf16 x, __bf16 (&p)[1]) { p[0] = x; }
+};
+template <> struct Parts<_Float16> {
+    static constexpr int count = 2;
+    static __device__ inline void split(_Float16 h, __bf16 (&p)[2])
+    {
+        const float x = (float)h;
+        p[0] = (__bf16)x;
+        p[1] = (__bf16)(finite_bits(x) ? x - (float)p[0] : 0.0f);
+    }
+};
+template <> struct Parts<float> {
+    static constexpr int count = 3;
+    static __device__ inline float cut(float x) { return __uint_as_float(__float_as_uint(x) & 0xFFFF0000u); }
+    static __device__ inline void split(float x, __bf16 (&p)[3])
+    {
+        const bool finite = finite_bits(x) != 0;
+        const float first = finite ? cut(x) : x, rest = finite ? x - first : 0.0f, second = cut(rest);
+        p[0] = (__bf16)first, p[1] = (__bf16)second, p[2] = (__bf16)(rest - second);
+    }
+};
+
+// What the parts after the first are multiplied by: numbers without the infinities, which the first part meets (a later
+// part that is zero would make a NaN of one).
+typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
+__device__ inline bf16x8 without_infinities(bf16x8 x)
+{
+    u16x8 u = __builtin_bit_cast(u16x8, x);
+    u *= __builtin_elementwise_min((u16x8)((u & (unsigned short)0x7FFF) ^ (unsigned short)0x7F80), (u16x8)(unsigned short)1);
+    return __builtin_bit_cast(bf16x8, u);
 }
 
 // WY x WX waves share a tile of dY's columns by the table's, FY x FX instructions of 32 x 32 x 16 each, and kStep rows are a
@@ -515,38 +829,6 @@ __global__ __launch_bounds__(64 * WY * WX, FY * FX > 4 ? 1 : 2) void f8_gradient
         EF_DTYPE(dtype, T, store_piece<T>(acc, turn, lane, (T *)out + first_row * ldo + first_col, ldo, rows, cols));
 }
 
-// Sums of the parts, in their order.
-template <class T>
-__global__ __launch_bounds__(256) void f8_join_kernel(const float *partial, int parts, u32 rows, u32 columns, T *out, long long ldo)
-{
-    const u32 row = blockIdx.y, c = (blockIdx.x * 256 + threadIdx.x) * 4;
-    if (c >= columns) return;
-    typedef float Four __attribute__((ext_vector_type(4), aligned(4)));
-    const size_t step = (size_t)rows * columns;
-    const float *from = partial + (size_t)row * columns + c;
-    f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (c + 4 <= columns) {
-        for (int p = 0; p < parts; ++p) sum += (f32x4) * (const Four *)(from + p * step);
-        T *o = out + (size_t)row * ldo + c;
-        typedef T Out __attribute__((ext_vector_type(4), aligned(sizeof(T))));
-        *(Out *)o = Out{from_float<T>(sum[0]), from_float<T>(sum[1]), from_float<T>(sum[2]), from_float<T>(sum[3])};
-    } else
-        for (u32 i = c; i < columns; ++i) {
-            float one = 0.0f;
-            for (int p = 0; p < parts; ++p) one += from[p * step + i - c];
-            out[(size_t)row * ldo + i] = from_float<T>(one);
-        }
-}
-
-template <class T>
-int launch_join(const float *partial, int parts, int64_t rows, int64_t columns, T *out, int64_t ldo, hipStream_t st)
-{
-    const dim3 grid((unsigned)((columns + 1023) / 1024), (unsigned)rows);
-    f8_join_kernel<T><<<grid, 256, 0, st>>>(partial, parts, (u32)rows, (u32)columns, out, ldo);
-    EF_HIP_CHECK(hipGetLastError());
-    return EFANNA_OK;
-}
-
 // Tiles of 128 or 256 a side, and as many parts of the sum as fill the GPU.
 struct GradientShape {
     int side, parts;
@@ -658,7 +940,11 @@ extern "C" int efanna_f8_rows(const uint8_t *codes, const uint8_t *scales, int32
     return EFANNA_OK;
 }
 
-extern "C" size_t efanna_f8_product_workspace_bytes(int64_t m, int64_t n, int32_t d) { return 0; }
+extern "C" size_t efanna_f8_product_workspace_bytes(int64_t m, int64_t n, int32_t d)
+{
+    if (m < 1 || m > kMaxRows || n < 1 || n > kMaxRows || d < 1 || d > EFANNA_F8_MAX_D) return 0;
+    return product_shape(m, n, d).bytes;
+}
 
 extern "C" int efanna_f8_product(const uint8_t *a_codes, const uint8_t *a_scales, int32_t a_format, int64_t m,
                                  const uint8_t *b_codes, const uint8_t *b_scales, int32_t b_format, int64_t n, int32_t d,
@@ -668,15 +954,19 @@ extern "C" int efanna_f8_product(const uint8_t *a_codes, const uint8_t *a_scales
         return EFANNA_EINVAL;
     if (m == 0 || n == 0) return EFANNA_OK;
     if (!out || !aligned_for(out, dtype)) return EFANNA_EINVAL;
-    if (!workspace_ok(ws, ws_bytes, efanna_f8_product_workspace_bytes(m, n, d))) return EFANNA_EWORKSPACE;
+    const ProductShape sh = product_shape(m, n, d);
+    if (!workspace_ok(ws, ws_bytes, sh.bytes)) return EFANNA_EWORKSPACE;
+    hipStream_t st = (hipStream_t)stream;
     const int nb = f8_blocks(d), sp = f8_scale_pitch(d);
     const F8 a = {a_codes, a_scales, (int)m, nb, sp}, b = {b_codes, b_scales, (int)n, nb, sp};
-    const int64_t tiles_b = (n + 31) / 32, tiles = (m + 31) / 32 * tiles_b;
-    if (tiles > 2147483647LL || !launch_fits((tiles + 3) / 4, 256)) return EFANNA_EUNSUPPORTED;
-    EF_DTYPE(dtype, T, EF_FORMAT(a_format, FA, EF_FORMAT(b_format, FB, (f8_product_kernel<T, FA, FB><<<(unsigned)((tiles + 3) / 4), 256, 0, (hipStream_t)stream>>>(
-                           a, b, (T *)out, ldo, (int)tiles_b, (u32)tiles)))));
-    EF_HIP_CHECK(hipGetLastError());
-    return EFANNA_OK;
+    int rc = EFANNA_OK;
+    EF_FORMAT(a_format, FA, EF_FORMAT(b_format, FB, {
+        if (dtype == EFANNA_F32) rc = launch_product<true, FA, FB>(a, b, dtype, out, ldo, sh, (float *)ws, st);
+        else rc = launch_product<false, FA, FB>(a, b, dtype, out, ldo, sh, (float *)ws, st);
+    }));
+    if (rc != EFANNA_OK || sh.parts == 1) return rc;
+    EF_DTYPE(dtype, T, rc = launch_join<T>((const float *)ws, sh.parts, m, n, (T *)out, ldo, st));
+    return rc;
 }
 
 extern "C" size_t efanna_f8_gradient_workspace_bytes(int64_t m, int32_t n, int32_t d)
