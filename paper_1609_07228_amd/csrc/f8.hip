@@ -645,25 +645,32 @@ int launch_product(const F8 &a, const F8 &b, int dtype, void *out, int64_t ldo, 
 template <class Y> struct Parts;
 template <> struct Parts<__bf16> {
     static constexpr int count = 1;
-    static __device__ inline void split(__bf16 x, __bf16 (&p)[1]) { p[0] = x; }
+    template <class Eight> static __device__ inline void split(Eight x, bf16x8 (&p)[1]) { p[0] = (bf16x8)x; }
 };
 template <> struct Parts<_Float16> {
     static constexpr int count = 2;
-    static __device__ inline void split(_Float16 h, __bf16 (&p)[2])
+    template <class Eight> static __device__ inline void split(Eight h, bf16x8 (&p)[2])
     {
-        const float x = (float)h;
-        p[0] = (__bf16)x;
-        p[1] = (__bf16)(finite_bits(x) ? x - (float)p[0] : 0.0f);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float x = (float)h[k];
+            p[0][k] = (__bf16)x;
+            p[1][k] = (__bf16)(finite_bits(x) ? x - (float)p[0][k] : 0.0f);
+        }
     }
 };
 template <> struct Parts<float> {
     static constexpr int count = 3;
     static __device__ inline float cut(float x) { return __uint_as_float(__float_as_uint(x) & 0xFFFF0000u); }
-    static __device__ inline void split(float x, __bf16 (&p)[3])
+    template <class Eight> static __device__ inline void split(Eight v, bf16x8 (&p)[3])
     {
-        const bool finite = finite_bits(x) != 0;
-        const float first = finite ? cut(x) : x, rest = finite ? x - first : 0.0f, second = cut(rest);
-        p[0] = (__bf16)first, p[1] = (__bf16)second, p[2] = (__bf16)(rest - second);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float x = v[k];
+            const bool finite = finite_bits(x) != 0;
+            const float first = finite ? cut(x) : x, rest = finite ? x - first : 0.0f, second = cut(rest);
+            p[0][k] = (__bf16)first, p[1][k] = (__bf16)second, p[2][k] = (__bf16)(rest - second);
+        }
     }
 };
 
@@ -677,93 +684,96 @@ __device__ inline bf16x8 without_infinities(bf16x8 x)
     return __builtin_bit_cast(bf16x8, u);
 }
 
-// WY x WX waves share a tile of dY's columns by the table's, FY x FX instructions of 32 x 32 x 16 each, and kStep rows are a
+// WY x WX waves share a tile of dY's columns by the table's, FY x FX instructions of 32 x 32 x 16 each, and STEP rows are a
 // stage.  Both operands are wanted by columns and lie in rows: rows go to LDS as bfloat16 numbers (dY in its parts, codes with
-// their scale applied, through registers: a stage is loaded while the one before the last is multiplied) and come back through
-// transposing reads, of which a lane gets four rows' values of its column.  A row's pieces of 16 columns (32 bytes) lie in the
-// order u ^ kTurn(row), so that the eight rows that a read touches are in different banks.
-constexpr int kStep = 32;
+// their scale applied, through registers, where AHEAD stages are on their way) and come back through transposing reads, of which a
+// lane gets four rows' values of its column.  A row's pieces of 16 columns (32 bytes) lie in the order u ^ turn_of(row), so that the
+// eight rows that a read touches are in different banks.
 __device__ inline int turn_of(int row) { return 2 * (row & 3) + ((row >> 2) & 1); }
 
-template <class Y, int FY, int FX, int WY, int WX>
+template <class Y, int FY, int FX, int WY, int WX, int STEP>
 struct GradientTile {
     static constexpr int waves = WY * WX, threads = 64 * waves, across_y = 32 * FY * WY, across_x = 32 * FX * WX, parts = Parts<Y>::count;
-    static constexpr int pieces_y = across_y / 8 * kStep / threads, pieces_x = across_x / 16 * kStep / threads;      // of a thread
-    static_assert(pieces_y * threads * 8 == across_y * kStep && pieces_x * threads * 16 == across_x * kStep, "every thread loads as much");
+    static constexpr int pieces_y = across_y / 8 * STEP / threads, pieces_x = across_x / 16 * STEP / threads;      // of a thread
+    static_assert(pieces_y * threads * 8 == across_y * STEP && pieces_x * threads * 16 == across_x * STEP, "every thread loads as much");
     struct Lds {
-        __bf16 y[2][parts][kStep][across_y], x[2][kStep][across_x];
+        __bf16 y[2][parts][STEP][across_y], x[2][STEP][across_x];
     };
     static constexpr int turn_bytes = 32 * (32 * FX + 8) * 4;        // of a wave, at the end
     static constexpr int lds = (int)sizeof(Lds) > waves * turn_bytes ? (int)sizeof(Lds) : waves * turn_bytes;
 };
 
 typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef short i16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
 
-template <class Y, int FORMAT, int FY, int FX, int WY, int WX>
+template <class Y, int FORMAT, int FY, int FX, int WY, int WX, int STEP, int AHEAD>
 __global__ __launch_bounds__(64 * WY * WX, FY * FX > 4 ? 1 : 2) void f8_gradient_kernel(const Y *dy, long long ldy, long long m, int n, F8 x, int d,
                                                                                        int dtype, void *out, long long ldo, int tiles_y,
                                                                                        int tiles_x, int parts, float *partial)
 {
-    typedef GradientTile<Y, FY, FX, WY, WX> Tile;
+    typedef GradientTile<Y, FY, FX, WY, WX, STEP> Tile;
     typedef Y Eight __attribute__((ext_vector_type(8), aligned(sizeof(Y))));
     extern __shared__ __align__(16) char lds_raw[];
     typename Tile::Lds &lds = *(typename Tile::Lds *)lds_raw;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
     const Place at = place_of(blockIdx.x, tiles_y, tiles_x, parts);
     const int j0 = at.y * Tile::across_y, c0 = at.x * Tile::across_x;
-    const int stages = (int)((m + kStep - 1) / kStep), s_lo = (int)((long long)stages * at.part / parts),
-              s_hi = (int)((long long)stages * (at.part + 1) / parts);
+    const long long all = (m + STEP - 1) / STEP, s_lo = all * at.part / parts, first = s_lo * STEP;
+    const int stages = (int)(all * (at.part + 1) / parts - s_lo);
+    const int rows_in = (int)min(m - first, (long long)stages * STEP);      // this part's rows: 0 .. rows_in - 1 from `first` on
 
-    Eight raw_y[Tile::pieces_y];
-    i32x4 raw_x[Tile::pieces_x];
-    u32 raw_scale[Tile::pieces_x];
-    const auto load = [&](int stage) {
+    // A stage on its way.  Rows past the last one are loaded from it and put down as zeros.
+    Eight raw_y[AHEAD][Tile::pieces_y];
+    i32x4 raw_x[AHEAD][Tile::pieces_x];
+    u32 raw_scale[AHEAD][Tile::pieces_x];
+    const Y *dy0 = dy + first * ldy + j0;
+    const uint8_t *codes0 = x.row(first), *scales0 = x.scales + (size_t)first * x.sp;
+    const auto load_y = [&](int stage, int set, int i) {
+        const int p = tid + Tile::threads * i, col = p % (Tile::across_y / 8) * 8;
+        const Y *from = dy0 + min(stage * STEP + p / (Tile::across_y / 8), rows_in - 1) * ldy;
+        if (j0 + col + 8 <= n) raw_y[set][i] = *(const Eight *)(from + col);
+        else {
+            int at = col;
+            asm volatile("" : "+v"(at));        // (or else eight offsets for each piece stay in registers)
 #pragma unroll
-        for (int i = 0; i < Tile::pieces_y; ++i) {
-            const int p = tid + Tile::threads * i, col = j0 + p % (Tile::across_y / 8) * 8;
-            const Y *from = dy + min((long long)stage * kStep + p / (Tile::across_y / 8), m - 1) * ldy;
-            if (col + 8 <= n) raw_y[i] = *(const Eight *)(from + col);
-            else
-#pragma unroll
-                for (int k = 0; k < 8; ++k) raw_y[i][k] = from[min(col + k, n - 1)];        // (columns past the last one are not stored)
-        }
-#pragma unroll
-        for (int i = 0; i < Tile::pieces_x; ++i) {
-            const int p = tid + Tile::threads * i, piece = min(c0 / 16 + p % (Tile::across_x / 16), x.nb * 8 - 1);
-            const long long row = min((long long)stage * kStep + p / (Tile::across_x / 16), m - 1);
-            raw_x[i] = *(const i32x4 *)(x.row(row) + piece * 16);
-            raw_scale[i] = x.scales[(size_t)row * x.sp + (piece >> 3)];
+            for (int k = 0; k < 8; ++k) raw_y[set][i][k] = from[min(at + k, n - 1 - j0)];        // (columns past the last one are not stored)
         }
     };
-    const auto put = [&](int stage) {
-        const int buffer = stage & 1;
+    const auto load_x = [&](int stage, int set, int i) {
+        const int p = tid + Tile::threads * i, piece = min(c0 / 16 + p % (Tile::across_x / 16), x.nb * 8 - 1);
+        const size_t row = min(stage * STEP + p / (Tile::across_x / 16), rows_in - 1);
+        raw_x[set][i] = *(const i32x4 *)(codes0 + row * x.nb * 128 + piece * 16);
+        raw_scale[set][i] = scales0[row * x.sp + (piece >> 3)];
+    };
+    const auto put_y = [&](int stage, int set, int buffer, int i) {
+        const int p = tid + Tile::threads * i, piece = p % (Tile::across_y / 8), row = p / (Tile::across_y / 8);
+        const bool live = stage * STEP + row < rows_in;
+        bf16x8 part[Tile::parts];
+        Parts<Y>::split(live ? raw_y[set][i] : (Eight)(Y)0.0f, part);
 #pragma unroll
-        for (int i = 0; i < Tile::pieces_y; ++i) {
-            const int p = tid + Tile::threads * i, piece = p % (Tile::across_y / 8), row = p / (Tile::across_y / 8);
-            const bool live = (long long)stage * kStep + row < m;
-            bf16x8 part[Tile::parts];
+        for (int q = 0; q < Tile::parts; ++q) *(bf16x8 *)&lds.y[buffer][q][row][((piece >> 1) ^ turn_of(row)) * 16 + (piece & 1) * 8] = part[q];
+    };
+    const auto put_x = [&](int stage, int set, int buffer, int i) {
+        const int p = tid + Tile::threads * i, piece = p % (Tile::across_x / 16), row = p / (Tile::across_x / 16);
+        const bool live = stage * STEP + row < rows_in;
+        bf16x8 wide[2];
+        sixteen_wide<FORMAT>(live ? raw_x[set][i] : i32x4{0, 0, 0, 0}, scale_value(live ? raw_scale[set][i] : 127), wide);
+        __bf16 *to = &lds.x[buffer][row][(piece ^ turn_of(row)) * 16];
+        *(bf16x8 *)to = wide[0];
+        *(bf16x8 *)(to + 8) = wide[1];
+    };
+    const auto load = [&](int stage, int set) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                __bf16 one[Tile::parts];
-                Parts<Y>::split(live ? raw_y[i][k] : (Y)0.0f, one);
+        for (int i = 0; i < Tile::pieces_x; ++i) load_x(stage, set, i);
 #pragma unroll
-                for (int q = 0; q < Tile::parts; ++q) part[q][k] = one[q];
-            }
+        for (int i = 0; i < Tile::pieces_y; ++i) load_y(stage, set, i);
+    };
+    const auto put = [&](int stage, int set, int buffer) {
 #pragma unroll
-            for (int q = 0; q < Tile::parts; ++q)
-                *(bf16x8 *)&lds.y[buffer][q][row][((piece >> 1) ^ turn_of(row)) * 16 + (piece & 1) * 8] = part[q];
-        }
+        for (int i = 0; i < Tile::pieces_x; ++i) put_x(stage, set, buffer, i);
 #pragma unroll
-        for (int i = 0; i < Tile::pieces_x; ++i) {
-            const int p = tid + Tile::threads * i, piece = p % (Tile::across_x / 16), row = p / (Tile::across_x / 16);
-            const bool live = (long long)stage * kStep + row < m;
-            bf16x8 wide[2];
-            sixteen_wide<FORMAT>(live ? raw_x[i] : i32x4{0, 0, 0, 0}, scale_value(live ? raw_scale[i] : 127), wide);
-            __bf16 *to = &lds.x[buffer][row][(piece ^ turn_of(row)) * 16];
-            *(bf16x8 *)to = wide[0];
-            *(bf16x8 *)(to + 8) = wide[1];
-        }
+        for (int i = 0; i < Tile::pieces_y; ++i) put_y(stage, set, buffer, i);
     };
 
     f32x16 acc[FY][FX] = {};
@@ -775,51 +785,75 @@ __global__ __launch_bounds__(64 * WY * WX, FY * FX > 4 ? 1 : 2) void f8_gradient
     for (int f = 0; f < FY; ++f) at_y[f] = row * Tile::across_y + (((wy * FY + f) * 2 + group) ^ turn_of(row)) * 16 + quarter;
 #pragma unroll
     for (int f = 0; f < FX; ++f) at_x[f] = row * Tile::across_x + (((wx * FX + f) * 2 + group) ^ turn_of(row)) * 16 + quarter;
-    const auto columns = [](const __bf16 *first, int pitch) {      // sixteen rows' values of the lane's column, as an operand
-        const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)first);
-        const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(first + 8 * pitch));
-        typedef short i16x8 __attribute__((ext_vector_type(8)));
+    const auto columns = [](const __bf16 *from, int pitch) {      // sixteen rows' values of the lane's column, as an operand
+        const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)from);
+        const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(from + 8 * pitch));
         return __builtin_bit_cast(bf16x8, (i16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     };
-    const auto multiply = [&](int stage) {
-        const int buffer = stage & 1;
+    // A stage is kUnits pieces of work, sixteen rows and a part of dY each; the next one's operands are read before one is done.
+    constexpr int kUnits = STEP / 16 * Tile::parts;
+    bf16x8 fx[2][FX], fy[2][FY];
+    const auto read = [&](int buffer, int unit, int to) {
+        const int k = unit / Tile::parts * 16, q = unit % Tile::parts;
+        if (q == 0)
 #pragma unroll
-        for (int k = 0; k < kStep; k += 16) {
-            bf16x8 fx[FX], fx_finite[FX];
+            for (int f = 0; f < FX; ++f) fx[unit / Tile::parts & 1][f] = columns(&lds.x[buffer][k][0] + at_x[f], Tile::across_x);
 #pragma unroll
-            for (int f = 0; f < FX; ++f) {
-                fx[f] = columns(&lds.x[buffer][k][0] + at_x[f], Tile::across_x);
-                if (Tile::parts > 1) fx_finite[f] = without_infinities(fx[f]);
-            }
+        for (int f = 0; f < FY; ++f) fy[to][f] = columns(&lds.y[buffer][q][k][0] + at_y[f], Tile::across_y);
+    };
+    const auto multiply = [&](int unit, int from) {
+        const int q = unit % Tile::parts, k = unit / Tile::parts & 1;
+        if (q == 1)
 #pragma unroll
-            for (int q = 0; q < Tile::parts; ++q) {
-                bf16x8 fy[FY];
+            for (int b = 0; b < FX; ++b) fx[k][b] = without_infinities(fx[k][b]);
 #pragma unroll
-                for (int f = 0; f < FY; ++f) fy[f] = columns(&lds.y[buffer][q][k][0] + at_y[f], Tile::across_y);
+        for (int a = 0; a < FY; ++a)
 #pragma unroll
-                for (int a = 0; a < FY; ++a)
-#pragma unroll
-                    for (int b = 0; b < FX; ++b)
-                        acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q ? fx_finite[b] : fx[b], fy[a], acc[a][b], 0, 0, 0);
-            }
-        }
+            for (int b = 0; b < FX; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[k][b], fy[from][a], acc[a][b], 0, 0, 0);
     };
     const auto meet = [&]() {          // what was written to LDS is there, what was read has arrived
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
-    if (s_lo < s_hi) {
-        load(s_lo);
-        put(s_lo);
-        if (s_lo + 1 < s_hi) load(s_lo + 1);
+    if (stages > 0) {
+        load(0, 0);
+        put(0, 0, 0);
+#pragma unroll
+        for (int s = 1; s <= AHEAD; ++s) load(s, s % AHEAD);
         meet();
-        for (int stage = s_lo; stage < s_hi; ++stage) {
-            if (stage + 1 < s_hi) put(stage + 1);
-            if (stage + 2 < s_hi) load(stage + 2);
-            multiply(stage);
-            meet();
+        read(0, 0, 0);
+        static_assert(kUnits % 2 == 0 && AHEAD <= 2, "operands and sets alternate");
+        for (int stage = 0;; stage += 2) {
+#pragma unroll
+            for (int odd = 0; odd < 2; ++odd) {
+#pragma unroll
+                for (int u = 0; u < kUnits - 1; ++u) {
+                    read(odd, u + 1, (u + 1) & 1);
+                    multiply(u, u & 1);
+                    // the next stage is put down and another one asked for, a share of it after each piece of work but the last
+                    constexpr int kPieces = Tile::pieces_x + Tile::pieces_y;
+                    const int set = (odd + 1) % AHEAD;
+#pragma unroll
+                    for (int i = kPieces * u / (kUnits - 1); i < kPieces * (u + 1) / (kUnits - 1); ++i)
+                        if (i < Tile::pieces_x) {
+                            put_x(stage + odd + 1, set, 1 - odd, i);
+                            load_x(stage + odd + 1 + AHEAD, set, i);
+                        } else {
+                            put_y(stage + odd + 1, set, 1 - odd, i - Tile::pieces_x);
+                            load_y(stage + odd + 1 + AHEAD, set, i - Tile::pieces_x);
+                        }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                meet();
+                if (stage + odd + 1 < stages) read(1 - odd, 0, 0);
+                multiply(kUnits - 1, 1);
+                __builtin_amdgcn_sched_barrier(0);
+                if (stage + odd + 1 >= stages) goto done;
+            }
         }
+    done:
+        meet();
     }
     const int rows = n - j0 - wy * FY * 32, cols = d - c0 - wx * FX * 32;
     const size_t first_row = j0 + wy * FY * 32, first_col = c0 + wx * FX * 32;
@@ -839,22 +873,22 @@ inline GradientShape gradient_shape(int64_t m, int32_t n, int32_t d)
     const auto tiles = [&](int side) { return (int64_t)((n + side - 1) / side) * ((d + side - 1) / side); };
     GradientShape s;
     s.side = tiles(256) >= 192 ? 256 : 128;
-    const int64_t room = s.side == 256 ? 256 : 512, stages = (m + kStep - 1) / kStep;
+    const int64_t room = s.side == 256 ? 256 : 512, stages = (m + 63) / 64;
     int64_t parts = room / tiles(s.side);
-    if (parts > stages / 8) parts = stages / 8;
+    if (parts > stages / 2) parts = stages / 2;
     s.parts = parts < 1 ? 1 : (int)parts;
     s.bytes = s.parts > 1 ? align_up((size_t)s.parts * n * d * sizeof(float)) : 0;
     return s;
 }
 
-template <class Y, int FORMAT, int FY, int FX, int WY, int WX>
+template <class Y, int FORMAT, int FY, int FX, int WY, int WX, int STEP, int AHEAD>
 int launch_gradient(const Y *dy, int64_t ldy, int64_t m, int n, const F8 &x, int d, int dtype, void *out, int64_t ldo, int parts,
                     float *partial, hipStream_t st)
 {
-    typedef GradientTile<Y, FY, FX, WY, WX> Tile;
+    typedef GradientTile<Y, FY, FX, WY, WX, STEP> Tile;
     const int ty = (n + Tile::across_y - 1) / Tile::across_y, tx = (d + Tile::across_x - 1) / Tile::across_x;
-    EF_HIP_CHECK(allow_lds((const void *)f8_gradient_kernel<Y, FORMAT, FY, FX, WY, WX>, Tile::lds));
-    f8_gradient_kernel<Y, FORMAT, FY, FX, WY, WX><<<(unsigned)(ty * tx * parts), Tile::threads, Tile::lds, st>>>(
+    EF_HIP_CHECK(allow_lds((const void *)f8_gradient_kernel<Y, FORMAT, FY, FX, WY, WX, STEP, AHEAD>, Tile::lds));
+    f8_gradient_kernel<Y, FORMAT, FY, FX, WY, WX, STEP, AHEAD><<<(unsigned)(ty * tx * parts), Tile::threads, Tile::lds, st>>>(
         dy, ldy, m, n, x, d, dtype, out, ldo, ty, tx, parts, partial);
     EF_HIP_CHECK(hipGetLastError());
     return EFANNA_OK;
@@ -989,8 +1023,9 @@ extern "C" int efanna_f8_gradient(const void *dY, int32_t dtype, int64_t m, int3
     const F8 x = {codes, scales, (int)m, f8_blocks(d), f8_scale_pitch(d)};
     int rc = EFANNA_OK;
     EF_DTYPE(dtype, Y, EF_FORMAT(format, F, {
-        if (sh.side == 256) rc = launch_gradient<Y, F, 4, 2, 2, 4>((const Y *)dY, ldy, m, n, x, d, out_dtype, out, ldo, sh.parts, (float *)ws, st);
-        else rc = launch_gradient<Y, F, 2, 2, 2, 2>((const Y *)dY, ldy, m, n, x, d, out_dtype, out, ldo, sh.parts, (float *)ws, st);
+        constexpr int step = Parts<Y>::count == 1 ? 64 : 32, ahead = Parts<Y>::count == 2 ? 2 : 1;
+        if (sh.side == 256) rc = launch_gradient<Y, F, 4, 2, 2, 4, step, ahead>((const Y *)dY, ldy, m, n, x, d, out_dtype, out, ldo, sh.parts, (float *)ws, st);
+        else rc = launch_gradient<Y, F, 2, 2, 2, 2, step, ahead>((const Y *)dY, ldy, m, n, x, d, out_dtype, out, ldo, sh.parts, (float *)ws, st);
     }));
     if (rc != EFANNA_OK || sh.parts == 1) return rc;
     EF_DTYPE(out_dtype, T, rc = launch_join<T>((const float *)ws, sh.parts, n, d, (T *)out, ldo, st));
