@@ -29,6 +29,7 @@ extern "C" {
 #endif
 
 #define EFANNA_F8_MAX_D 65536
+#define EFANNA_F8_MAX_LDY 16777216   /* elements between the rows of a gradient: fewer */
 #define EFANNA_E4M3 0
 #define EFANNA_E5M2 1
 
@@ -72,6 +73,7 @@ int efanna_f8_product(const uint8_t *a_codes, const uint8_t *a_scales, int32_t a
  * coordinates).  ldo >= d; n <= EFANNA_F8_MAX_D; with m = 0 the sums are zeros.
  * Nothing is rounded but sums, in float32, and the result, to out_dtype (values of the table below 2^-126 count
  * in steps of 2^-133, those of dY are taken in parts, of which the ones below 2^-133 are lost).
+ * EFANNA_EUNSUPPORTED for ldy >= EFANNA_F8_MAX_LDY.
  * ws     [device] 256-byte aligned, efanna_f8_gradient_workspace_bytes bytes; may be NULL where that is 0. */
 size_t efanna_f8_gradient_workspace_bytes(int64_t m, int32_t n, int32_t d);
 

@@ -691,6 +691,9 @@ __device__ inline bf16x8 without_infinities(bf16x8 x)
 // eight rows that a read touches are in different banks.
 __device__ inline int turn_of(int row) { return 2 * (row & 3) + ((row >> 2) & 1); }
 
+// (a closure that is called twice and not inlined keeps what it captures, the accumulators too, in memory)
+#define EF_INLINE __attribute__((always_inline))
+
 template <class Y, int FY, int FX, int WY, int WX, int STEP>
 struct GradientTile {
     static constexpr int waves = WY * WX, threads = 64 * waves, across_y = 32 * FY * WY, across_x = 32 * FX * WX, parts = Parts<Y>::count;
@@ -723,57 +726,53 @@ __global__ __launch_bounds__(64 * WY * WX, FY * FX > 4 ? 1 : 2) void f8_gradient
     const int stages = (int)(all * (at.part + 1) / parts - s_lo);
     const int rows_in = (int)min(m - first, (long long)stages * STEP);      // this part's rows: 0 .. rows_in - 1 from `first` on
 
-    // A stage on its way.  Rows past the last one are loaded from it and put down as zeros.
+    // A stage on its way.  Rows past the last one are loaded from it and put down as zeros; a stage past the last is loaded again
+    // (nothing reads it).  Offsets within a stage are below 2^32.
     Eight raw_y[AHEAD][Tile::pieces_y];
     i32x4 raw_x[AHEAD][Tile::pieces_x];
     u32 raw_scale[AHEAD][Tile::pieces_x];
     const Y *dy0 = dy + first * ldy + j0;
     const uint8_t *codes0 = x.row(first), *scales0 = x.scales + (size_t)first * x.sp;
-    const auto load_y = [&](int stage, int set, int i) {
-        const int p = tid + Tile::threads * i, col = p % (Tile::across_y / 8) * 8;
-        const Y *from = dy0 + min(stage * STEP + p / (Tile::across_y / 8), rows_in - 1) * ldy;
-        if (j0 + col + 8 <= n) raw_y[set][i] = *(const Eight *)(from + col);
-        else {
-            int at = col;
-            asm volatile("" : "+v"(at));        // (or else eight offsets for each piece stay in registers)
+    const int col_y = tid % (Tile::across_y / 8) * 8, row_y = tid / (Tile::across_y / 8), rows_y = Tile::threads / (Tile::across_y / 8);
+    const int piece_x = min(c0 / 16 + tid % (Tile::across_x / 16), x.nb * 8 - 1), row_x = tid / (Tile::across_x / 16),
+              rows_x = Tile::threads / (Tile::across_x / 16);
+    const auto load_y = [&](int stage, int set, int i, auto inside) EF_INLINE {
+        const int at = min(stage, stages - 1) * STEP, row = min(row_y + rows_y * i, rows_in - 1 - at);
+        const Y *from = dy0 + at * ldy;
+        const u32 offset = (u32)row * (u32)ldy + col_y;
+        if (inside || j0 + col_y + 8 <= n) raw_y[set][i] = *(const Eight *)(from + offset);
+        else
 #pragma unroll
-            for (int k = 0; k < 8; ++k) raw_y[set][i][k] = from[min(at + k, n - 1 - j0)];        // (columns past the last one are not stored)
-        }
+            for (int k = 0; k < 8; ++k) raw_y[set][i][k] = from[(u32)row * (u32)ldy + min(col_y + k, n - 1 - j0)];        // (columns past the last one are not stored)
     };
-    const auto load_x = [&](int stage, int set, int i) {
-        const int p = tid + Tile::threads * i, piece = min(c0 / 16 + p % (Tile::across_x / 16), x.nb * 8 - 1);
-        const size_t row = min(stage * STEP + p / (Tile::across_x / 16), rows_in - 1);
-        raw_x[set][i] = *(const i32x4 *)(codes0 + row * x.nb * 128 + piece * 16);
-        raw_scale[set][i] = scales0[row * x.sp + (piece >> 3)];
+    const auto load_x = [&](int stage, int set, int i) EF_INLINE {
+        const int at = min(stage, stages - 1) * STEP, row = min(row_x + rows_x * i, rows_in - 1 - at);
+        raw_x[set][i] = *(const i32x4 *)(codes0 + (size_t)at * x.nb * 128 + ((u32)row * x.nb * 128 + piece_x * 16));
+        raw_scale[set][i] = *(const u32 *)(scales0 + (size_t)at * x.sp + ((u32)row * x.sp + (piece_x >> 5) * 4));
     };
-    const auto put_y = [&](int stage, int set, int buffer, int i) {
-        const int p = tid + Tile::threads * i, piece = p % (Tile::across_y / 8), row = p / (Tile::across_y / 8);
+    const int shift_x = 8 * ((piece_x >> 3) & 3);
+    const auto put_y = [&](int stage, int set, int buffer, int i) EF_INLINE {
+        const int piece = col_y / 8, row = row_y + rows_y * i;
         const bool live = stage * STEP + row < rows_in;
         bf16x8 part[Tile::parts];
         Parts<Y>::split(live ? raw_y[set][i] : (Eight)(Y)0.0f, part);
 #pragma unroll
         for (int q = 0; q < Tile::parts; ++q) *(bf16x8 *)&lds.y[buffer][q][row][((piece >> 1) ^ turn_of(row)) * 16 + (piece & 1) * 8] = part[q];
     };
-    const auto put_x = [&](int stage, int set, int buffer, int i) {
-        const int p = tid + Tile::threads * i, piece = p % (Tile::across_x / 16), row = p / (Tile::across_x / 16);
+    const auto put_x = [&](int stage, int set, int buffer, int i) EF_INLINE {
+        const int piece = tid % (Tile::across_x / 16), row = row_x + rows_x * i;
         const bool live = stage * STEP + row < rows_in;
         bf16x8 wide[2];
-        sixteen_wide<FORMAT>(live ? raw_x[set][i] : i32x4{0, 0, 0, 0}, scale_value(live ? raw_scale[set][i] : 127), wide);
-        __bf16 *to = &lds.x[buffer][row][(piece ^ turn_of(row)) * 16];
+        u32 word = raw_scale[set][i];
+        asm volatile("" : "+v"(word));
+        const u32 scale = (word >> shift_x) & 255;
+        // (the second four lanes of eight write their second half first: a write's 16 bytes per lane are in different banks)
+        const bool swap = tid & 4;
+        const i32x4 c = live ? raw_x[set][i] : i32x4{0, 0, 0, 0};
+        sixteen_wide<FORMAT>(swap ? i32x4{c.z, c.w, c.x, c.y} : c, scale_value(live ? scale : 127), wide);
+        __bf16 *to = &lds.x[buffer][row][(piece ^ turn_of(row)) * 16 + (swap ? 8 : 0)];
         *(bf16x8 *)to = wide[0];
-        *(bf16x8 *)(to + 8) = wide[1];
-    };
-    const auto load = [&](int stage, int set) {
-#pragma unroll
-        for (int i = 0; i < Tile::pieces_x; ++i) load_x(stage, set, i);
-#pragma unroll
-        for (int i = 0; i < Tile::pieces_y; ++i) load_y(stage, set, i);
-    };
-    const auto put = [&](int stage, int set, int buffer) {
-#pragma unroll
-        for (int i = 0; i < Tile::pieces_x; ++i) put_x(stage, set, buffer, i);
-#pragma unroll
-        for (int i = 0; i < Tile::pieces_y; ++i) put_y(stage, set, buffer, i);
+        *(bf16x8 *)(to + (swap ? -8 : 8)) = wide[1];
     };
 
     f32x16 acc[FY][FX] = {};
@@ -793,7 +792,7 @@ __global__ __launch_bounds__(64 * WY * WX, FY * FX > 4 ? 1 : 2) void f8_gradient
     // A stage is kUnits pieces of work, sixteen rows and a part of dY each; the next one's operands are read before one is done.
     constexpr int kUnits = STEP / 16 * Tile::parts;
     bf16x8 fx[2][FX], fy[2][FY];
-    const auto read = [&](int buffer, int unit, int to) {
+    const auto read = [&](int buffer, int unit, int to) EF_INLINE {
         const int k = unit / Tile::parts * 16, q = unit % Tile::parts;
         if (q == 0)
 #pragma unroll
@@ -801,7 +800,7 @@ __global__ __launch_bounds__(64 * WY * WX, FY * FX > 4 ? 1 : 2) void f8_gradient
 #pragma unroll
         for (int f = 0; f < FY; ++f) fy[to][f] = columns(&lds.y[buffer][q][k][0] + at_y[f], Tile::across_y);
     };
-    const auto multiply = [&](int unit, int from) {
+    const auto multiply = [&](int unit, int from) EF_INLINE {
         const int q = unit % Tile::parts, k = unit / Tile::parts & 1;
         if (q == 1)
 #pragma unroll
@@ -816,14 +815,28 @@ __global__ __launch_bounds__(64 * WY * WX, FY * FX > 4 ? 1 : 2) void f8_gradient
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
-    if (stages > 0) {
-        load(0, 0);
-        put(0, 0, 0);
+    static_assert(kUnits % 2 == 0 && AHEAD <= 2, "operands and sets alternate");
+    static_assert(kUnits % 2 == 0 && AHEAD <= 2, "operands and sets alternate");
+    constexpr int kPieces = Tile::pieces_x + Tile::pieces_y;
+    const auto run = [&](auto inside) EF_INLINE {      // INSIDE: whole pieces of dY, without a look at where its rows end
+        const auto load = [&](int stage, int set, int i) EF_INLINE {
+            if (i < Tile::pieces_x) load_x(stage, set, i);
+            else load_y(stage, set, i - Tile::pieces_x, inside);
+        };
+        const auto put = [&](int stage, int set, int buffer, int i) EF_INLINE {
+            if (i < Tile::pieces_x) put_x(stage, set, buffer, i);
+            else put_y(stage, set, buffer, i - Tile::pieces_x);
+        };
 #pragma unroll
-        for (int s = 1; s <= AHEAD; ++s) load(s, s % AHEAD);
+        for (int i = 0; i < kPieces; ++i) load(0, 0, i);
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) put(0, 0, 0, i);
+#pragma unroll
+        for (int s = 1; s <= AHEAD; ++s)
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) load(s, s % AHEAD, i);
         meet();
         read(0, 0, 0);
-        static_assert(kUnits % 2 == 0 && AHEAD <= 2, "operands and sets alternate");
         for (int stage = 0;; stage += 2) {
 #pragma unroll
             for (int odd = 0; odd < 2; ++odd) {
@@ -831,28 +844,35 @@ __global__ __launch_bounds__(64 * WY * WX, FY * FX > 4 ? 1 : 2) void f8_gradient
                 for (int u = 0; u < kUnits - 1; ++u) {
                     read(odd, u + 1, (u + 1) & 1);
                     multiply(u, u & 1);
-                    // the next stage is put down and another one asked for, a share of it after each piece of work but the last
-                    constexpr int kPieces = Tile::pieces_x + Tile::pieces_y;
-                    const int set = (odd + 1) % AHEAD;
+                    // the next stage is put down and another one asked for, a share of it with each piece of work but the last
 #pragma unroll
-                    for (int i = kPieces * u / (kUnits - 1); i < kPieces * (u + 1) / (kUnits - 1); ++i)
-                        if (i < Tile::pieces_x) {
-                            put_x(stage + odd + 1, set, 1 - odd, i);
-                            load_x(stage + odd + 1 + AHEAD, set, i);
-                        } else {
-                            put_y(stage + odd + 1, set, 1 - odd, i - Tile::pieces_x);
-                            load_y(stage + odd + 1 + AHEAD, set, i - Tile::pieces_x);
-                        }
+                    for (int i = kPieces * u / (kUnits - 1); i < kPieces * (u + 1) / (kUnits - 1); ++i) {
+                        put(stage + odd + 1, (odd + 1) % AHEAD, 1 - odd, i);
+                        load(stage + odd + 1 + AHEAD, (odd + 1) % AHEAD, i);
+                    }
+                    // (between two matrix instructions there is room for so many others)
+#pragma unroll
+                    for (int i = 0; i < FY * FX; ++i) {
+                        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);      // matrix
+                        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);      // reads of LDS
+                        __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);      // vector
+                        __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);      // writes of LDS
+                        __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+                        __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);      // loads
+                    }
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 meet();
-                if (stage + odd + 1 < stages) read(1 - odd, 0, 0);
+                read(1 - odd, 0, 0);                  // (after the last stage: what was put down as one past it)
                 multiply(kUnits - 1, 1);
                 __builtin_amdgcn_sched_barrier(0);
-                if (stage + odd + 1 >= stages) goto done;
+                if (stage + odd + 1 >= stages) return;
             }
         }
-    done:
+    };
+    if (stages > 0) {
+        if (j0 + Tile::across_y <= n) run(std::true_type());
+        else run(std::false_type());
         meet();
     }
     const int rows = n - j0 - wy * FY * 32, cols = d - c0 - wx * FX * 32;
@@ -1016,6 +1036,7 @@ extern "C" int efanna_f8_gradient(const void *dY, int32_t dtype, int64_t m, int3
     if (!dtype_ok(dtype) || !dtype_ok(out_dtype) || !table_ok(codes, scales, format, m, d) || n < 0 || n > EFANNA_F8_MAX_D || ldy < n || ldo < d)
         return EFANNA_EINVAL;
     if (n == 0) return EFANNA_OK;
+    if (ldy >= EFANNA_F8_MAX_LDY) return EFANNA_EUNSUPPORTED;
     if ((m > 0 && !dY) || !out || !aligned_for(dY, dtype) || !aligned_for(out, out_dtype)) return EFANNA_EINVAL;
     const GradientShape sh = gradient_shape(m, n, d);
     if (!workspace_ok(ws, ws_bytes, sh.bytes)) return EFANNA_EWORKSPACE;
@@ -1023,9 +1044,9 @@ extern "C" int efanna_f8_gradient(const void *dY, int32_t dtype, int64_t m, int3
     const F8 x = {codes, scales, (int)m, f8_blocks(d), f8_scale_pitch(d)};
     int rc = EFANNA_OK;
     EF_DTYPE(dtype, Y, EF_FORMAT(format, F, {
-        constexpr int step = Parts<Y>::count == 1 ? 64 : 32, ahead = Parts<Y>::count == 2 ? 2 : 1;
-        if (sh.side == 256) rc = launch_gradient<Y, F, 4, 2, 2, 4, step, ahead>((const Y *)dY, ldy, m, n, x, d, out_dtype, out, ldo, sh.parts, (float *)ws, st);
-        else rc = launch_gradient<Y, F, 2, 2, 2, 2, step, ahead>((const Y *)dY, ldy, m, n, x, d, out_dtype, out, ldo, sh.parts, (float *)ws, st);
+        constexpr int ahead = Parts<Y>::count == 3 ? 1 : 2;
+        if (sh.side == 256) rc = launch_gradient<Y, F, 4, 2, 2, 4, 32, ahead>((const Y *)dY, ldy, m, n, x, d, out_dtype, out, ldo, sh.parts, (float *)ws, st);
+        else rc = launch_gradient<Y, F, 2, 2, 2, 2, 32, 2>((const Y *)dY, ldy, m, n, x, d, out_dtype, out, ldo, sh.parts, (float *)ws, st);
     }));
     if (rc != EFANNA_OK || sh.parts == 1) return rc;
     EF_DTYPE(out_dtype, T, rc = launch_join<T>((const float *)ws, sh.parts, n, d, (T *)out, ldo, st));
