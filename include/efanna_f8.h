@@ -75,7 +75,7 @@ int efanna_f8_product(const uint8_t *a_codes, const uint8_t *a_scales, int32_t a
  * in steps of 2^-133, those of dY are taken in parts, of which the ones below 2^-133 are lost).
  * EFANNA_EUNSUPPORTED for ldy >= EFANNA_F8_MAX_LDY.
  * ws     [device] 256-byte aligned, efanna_f8_gradient_workspace_bytes bytes; may be NULL where that is 0. */
-size_t efanna_f8_gradient_workspace_bytes(int64_t m, int32_t n, int32_t d);
+size_t efanna_f8_gradient_workspace_bytes(int64_t m, int32_t n, int32_t d, int32_t dtype);
 
 int efanna_f8_gradient(const void *dY, int32_t dtype, int64_t m, int32_t n, int64_t ldy, const uint8_t *codes,
                        const uint8_t *scales, int32_t format, int32_t d, int32_t out_dtype, void *out,

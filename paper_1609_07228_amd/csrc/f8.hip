@@ -292,33 +292,31 @@ __device__ inline Place place_of(u32 id, int tiles_y, int tiles_x, int parts)
     return {strip * 8 + in % high, in / high, part};
 }
 
-// Sums of the parts, in their order.
+// Sums of the parts, in their order: a lane per result, eight loads on their way.
 template <class T>
 __global__ __launch_bounds__(256) void f8_join_kernel(const float *partial, int parts, u32 rows, u32 columns, T *out, long long ldo)
 {
-    const u32 row = blockIdx.y, c = (blockIdx.x * 256 + threadIdx.x) * 4;
+    const u32 row = blockIdx.y, c = blockIdx.x * 256 + threadIdx.x;
     if (c >= columns) return;
-    typedef float Four __attribute__((ext_vector_type(4), aligned(4)));
     const size_t step = (size_t)rows * columns;
     const float *from = partial + (size_t)row * columns + c;
-    f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (c + 4 <= columns) {
-        for (int p = 0; p < parts; ++p) sum += (f32x4) * (const Four *)(from + p * step);
-        T *o = out + (size_t)row * ldo + c;
-        typedef T Out __attribute__((ext_vector_type(4), aligned(sizeof(T))));
-        *(Out *)o = Out{from_float<T>(sum[0]), from_float<T>(sum[1]), from_float<T>(sum[2]), from_float<T>(sum[3])};
-    } else
-        for (u32 i = c; i < columns; ++i) {
-            float one = 0.0f;
-            for (int p = 0; p < parts; ++p) one += from[p * step + i - c];
-            out[(size_t)row * ldo + i] = from_float<T>(one);
-        }
+    float sum = 0.0f;
+    int p = 0;
+    for (; p + 8 <= parts; p += 8, from += 8 * step) {
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = from[i * step];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += x[i];
+    }
+    for (; p < parts; ++p, from += step) sum += *from;
+    out[(size_t)row * ldo + c] = from_float<T>(sum);
 }
 
 template <class T>
 int launch_join(const float *partial, int parts, int64_t rows, int64_t columns, T *out, int64_t ldo, hipStream_t st)
 {
-    const dim3 grid((unsigned)((columns + 1023) / 1024), (unsigned)rows);
+    const dim3 grid((unsigned)((columns + 255) / 256), (unsigned)rows);
     f8_join_kernel<T><<<grid, 256, 0, st>>>(partial, parts, (u32)rows, (u32)columns, out, ldo);
     EF_HIP_CHECK(hipGetLastError());
     return EFANNA_OK;
@@ -640,38 +638,34 @@ int launch_product(const F8 &a, const F8 &b, int dtype, void *out, int64_t ldo, 
 }
 
 // ---- gradient of the weights -----------------------------------------------------------------------------
-// A number as a sum of bfloat16 numbers, exactly (from 2^-110 on for float32): one of its own kind, two of half precision (11
-// bits), three of float32 (24 bits).  Infinities and NaN are all in the first part.
-template <class Y> struct Parts;
+// A number as a sum of bfloat16 numbers, exactly (float32 from 2^-110 on): one of its own kind, two of half precision (11
+// bits), three of float32 (24 bits).  A part is the upper half of what is left as a float32 number, eight bits of it.  An
+// infinity is all in the first part.
+template <class Y> struct Parts {
+    static constexpr int count = sizeof(Y) == 4 ? 3 : 2;
+    template <class Eight> static __device__ inline void split(Eight v, bf16x8 (&p)[count])
+    {
+        u32 left[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) left[k] = __float_as_uint((float)v[k]);
+#pragma unroll
+        for (int q = 0; q < count; ++q) {
+            u32x4 halves;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) halves[k] = __builtin_amdgcn_perm(left[2 * k + 1], left[2 * k], 0x07060302);
+            p[q] = __builtin_bit_cast(bf16x8, halves);
+            if (q + 1 < count)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const float x = __uint_as_float(left[k]), rest = x - __uint_as_float(left[k] & 0xFFFF0000u);
+                    left[k] = __float_as_uint(q == 0 && __builtin_amdgcn_classf(x, 0x204) ? 0.0f : rest);
+                }
+        }
+    }
+};
 template <> struct Parts<__bf16> {
     static constexpr int count = 1;
     template <class Eight> static __device__ inline void split(Eight x, bf16x8 (&p)[1]) { p[0] = (bf16x8)x; }
-};
-template <> struct Parts<_Float16> {
-    static constexpr int count = 2;
-    template <class Eight> static __device__ inline void split(Eight h, bf16x8 (&p)[2])
-    {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const float x = (float)h[k];
-            p[0][k] = (__bf16)x;
-            p[1][k] = (__bf16)(finite_bits(x) ? x - (float)p[0][k] : 0.0f);
-        }
-    }
-};
-template <> struct Parts<float> {
-    static constexpr int count = 3;
-    static __device__ inline float cut(float x) { return __uint_as_float(__float_as_uint(x) & 0xFFFF0000u); }
-    template <class Eight> static __device__ inline void split(Eight v, bf16x8 (&p)[3])
-    {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const float x = v[k];
-            const bool finite = finite_bits(x) != 0;
-            const float first = finite ? cut(x) : x, rest = finite ? x - first : 0.0f, second = cut(rest);
-            p[0][k] = (__bf16)first, p[1][k] = (__bf16)second, p[2][k] = (__bf16)(rest - second);
-        }
-    }
 };
 
 // What the parts after the first are multiplied by: numbers without the infinities, which the first part meets (a later
@@ -711,7 +705,7 @@ typedef short i16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
 
 template <class Y, int FORMAT, int FY, int FX, int WY, int WX, int STEP, int AHEAD>
-__global__ __launch_bounds__(64 * WY * WX, FY * FX > 4 ? 1 : 2) void f8_gradient_kernel(const Y *dy, long long ldy, long long m, int n, F8 x, int d,
+__global__ __launch_bounds__(64 * WY * WX, 2) void f8_gradient_kernel(const Y *dy, long long ldy, long long m, int n, F8 x, int d,
                                                                                        int dtype, void *out, long long ldo, int tiles_y,
                                                                                        int tiles_x, int parts, float *partial)
 {
@@ -883,22 +877,42 @@ __global__ __launch_bounds__(64 * WY * WX, FY * FX > 4 ? 1 : 2) void f8_gradient
         EF_DTYPE(dtype, T, store_piece<T>(acc, turn, lane, (T *)out + first_row * ldo + first_col, ldo, rows, cols));
 }
 
-// Tiles of 128 or 256 a side, and as many parts of the sum as fill the GPU.
+// How a gradient is cut: which tile, and in how many parts the sum.  The larger tiles move half as much per operation, one at a time
+// on a CU; the wide one is for few columns of dY; two of the small ones run on a CU and leave half as many sums to be joined.  The
+// choice is the least of estimated times, from what the kernels were measured at.
+constexpr int kStep = 32;
+enum GradientKind { kSquare, kWide, kSmall };
 struct GradientShape {
-    int side, parts;
+    int kind, parts;
     size_t bytes;
 };
-inline GradientShape gradient_shape(int64_t m, int32_t n, int32_t d)
+inline GradientShape gradient_shape(int64_t m, int32_t n, int32_t d, int32_t dtype)
 {
-    const auto tiles = [&](int side) { return (int64_t)((n + side - 1) / side) * ((d + side - 1) / side); };
-    GradientShape s;
-    s.side = tiles(256) >= 192 ? 256 : 128;
-    const int64_t room = s.side == 256 ? 256 : 512, stages = (m + 63) / 64;
-    int64_t parts = room / tiles(s.side);
-    if (parts > stages / 2) parts = stages / 2;
-    s.parts = parts < 1 ? 1 : (int)parts;
-    s.bytes = s.parts > 1 ? align_up((size_t)s.parts * n * d * sizeof(float)) : 0;
-    return s;
+    struct Kind {
+        int y, x, at_once;             // sides, workgroups that run at once
+        double stage[3];               // microseconds, by parts of an element of dY
+    };
+    static const Kind kinds[3] = {{256, 256, 256, {0.95, 1.75, 3.2}}, {128, 512, 256, {1.05, 1.9, 2.9}}, {128, 128, 512, {0.75, 1.3, 2.1}}};
+    const int p = dtype == EFANNA_F32 ? 2 : dtype == EFANNA_F16 ? 1 : 0;
+    const int64_t stages = (m + kStep - 1) / kStep;
+    GradientShape best = {kSmall, 1, 0};
+    double least = 1e300;
+    for (int k = 0; k < 3; ++k) {
+        const int64_t tiles = (int64_t)((n + kinds[k].y - 1) / kinds[k].y) * ((d + kinds[k].x - 1) / kinds[k].x);
+        int64_t most = kinds[k].at_once / tiles;
+        if (most > stages / 2) most = stages / 2;
+        for (int64_t parts = 1; parts <= (most < 1 ? 1 : most); ++parts) {
+            const int64_t rounds = (tiles * parts + kinds[k].at_once - 1) / kinds[k].at_once;
+            const double alone = 2 * tiles * parts <= kinds[k].at_once && k == kSmall ? 0.65 : 1.0;      // a CU's only one
+            double time = rounds * (6.0 + (double)((stages + parts - 1) / parts) * kinds[k].stage[p] * alone);
+            if (parts > 1) time += 3.0 + (double)parts * n * d * 8.0 / 4e6;      // written and read again
+            if (time < least) {
+                least = time;
+                best = {k, (int)parts, parts > 1 ? align_up((size_t)parts * n * d * sizeof(float)) : 0};
+            }
+        }
+    }
+    return best;
 }
 
 template <class Y, int FORMAT, int FY, int FX, int WY, int WX, int STEP, int AHEAD>
@@ -1023,10 +1037,10 @@ extern "C" int efanna_f8_product(const uint8_t *a_codes, const uint8_t *a_scales
     return rc;
 }
 
-extern "C" size_t efanna_f8_gradient_workspace_bytes(int64_t m, int32_t n, int32_t d)
+extern "C" size_t efanna_f8_gradient_workspace_bytes(int64_t m, int32_t n, int32_t d, int32_t dtype)
 {
-    if (m < 0 || m > kMaxRows || n < 1 || n > EFANNA_F8_MAX_D || d < 1 || d > EFANNA_F8_MAX_D) return 0;
-    return gradient_shape(m, n, d).bytes;
+    if (m < 0 || m > kMaxRows || n < 1 || n > EFANNA_F8_MAX_D || d < 1 || d > EFANNA_F8_MAX_D || !dtype_ok(dtype)) return 0;
+    return gradient_shape(m, n, d, dtype).bytes;
 }
 
 extern "C" int efanna_f8_gradient(const void *dY, int32_t dtype, int64_t m, int32_t n, int64_t ldy, const uint8_t *codes,
@@ -1038,15 +1052,17 @@ extern "C" int efanna_f8_gradient(const void *dY, int32_t dtype, int64_t m, int3
     if (n == 0) return EFANNA_OK;
     if (ldy >= EFANNA_F8_MAX_LDY) return EFANNA_EUNSUPPORTED;
     if ((m > 0 && !dY) || !out || !aligned_for(dY, dtype) || !aligned_for(out, out_dtype)) return EFANNA_EINVAL;
-    const GradientShape sh = gradient_shape(m, n, d);
+    const GradientShape sh = gradient_shape(m, n, d, dtype);
     if (!workspace_ok(ws, ws_bytes, sh.bytes)) return EFANNA_EWORKSPACE;
     hipStream_t st = (hipStream_t)stream;
     const F8 x = {codes, scales, (int)m, f8_blocks(d), f8_scale_pitch(d)};
     int rc = EFANNA_OK;
     EF_DTYPE(dtype, Y, EF_FORMAT(format, F, {
         constexpr int ahead = Parts<Y>::count == 3 ? 1 : 2;
-        if (sh.side == 256) rc = launch_gradient<Y, F, 4, 2, 2, 4, 32, ahead>((const Y *)dY, ldy, m, n, x, d, out_dtype, out, ldo, sh.parts, (float *)ws, st);
-        else rc = launch_gradient<Y, F, 2, 2, 2, 2, 32, 2>((const Y *)dY, ldy, m, n, x, d, out_dtype, out, ldo, sh.parts, (float *)ws, st);
+        const auto run = sh.kind == kSquare ? launch_gradient<Y, F, 4, 2, 2, 4, kStep, ahead>
+                         : sh.kind == kWide ? launch_gradient<Y, F, 4, 2, 1, 8, kStep, ahead>
+                                            : launch_gradient<Y, F, 2, 2, 2, 2, kStep, 2>;
+        rc = run((const Y *)dY, ldy, m, n, x, d, out_dtype, out, ldo, sh.parts, (float *)ws, st);
     }));
     if (rc != EFANNA_OK || sh.parts == 1) return rc;
     EF_DTYPE(out_dtype, T, rc = launch_join<T>((const float *)ws, sh.parts, n, d, (T *)out, ldo, st));

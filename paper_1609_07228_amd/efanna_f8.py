@@ -40,7 +40,7 @@ def lib():
         L.efanna_f8_product.restype = C.c_int
         L.efanna_f8_product.argtypes = [vp, vp, i32, i64, vp, vp, i32, i64, i32, i32, vp, i64, vp, sz, vp]
         L.efanna_f8_gradient_workspace_bytes.restype = sz
-        L.efanna_f8_gradient_workspace_bytes.argtypes = [i64, i32, i32]
+        L.efanna_f8_gradient_workspace_bytes.argtypes = [i64, i32, i32, i32]
         L.efanna_f8_gradient.restype = C.c_int
         L.efanna_f8_gradient.argtypes = [vp, i32, i64, i32, i64, vp, vp, i32, i32, i32, vp, i64, vp, sz, vp]
         _known = L
@@ -165,7 +165,7 @@ def efanna_f8_gradient(dY: torch.Tensor, x: F8Table, dtype: torch.dtype = torch.
     n = dY.shape[1]
     out = _efanna._mx_out(out, (n, x.d), dtype, dY.device)
     ldo = out.stride(0) if n > 1 else x.d
-    at, size, _keep = _room(lib().efanna_f8_gradient_workspace_bytes(m, n, x.d), dY, workspace)
+    at, size, _keep = _room(lib().efanna_f8_gradient_workspace_bytes(m, n, x.d, kind), dY, workspace)
     _efanna._call("efanna_f8_gradient", dY, dY.data_ptr(), kind, m, n, ldy, x.codes.data_ptr(), x.scales.data_ptr(), form, x.d,
                   code, out.data_ptr(), ldo, at, size)
     return out

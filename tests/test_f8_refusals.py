@@ -9,7 +9,7 @@ import pytest
 torch = pytest.importorskip("torch")
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
-EINVAL, EWORKSPACE, OK = -1, -2, 0
+EINVAL, EWORKSPACE, EUNSUPPORTED, OK = -1, -2, -6, 0
 ONE = C.c_void_p(4096)          # never dereferenced: every call below fails, or has nothing to do
 ODD = C.c_void_p(4097)
 HALF = C.c_void_p(4098)
@@ -92,7 +92,7 @@ def test_product(f8):
 def test_gradient(f8):
     L = f8.lib()
     m, n, d = 100_000, 60, 40
-    need = L.efanna_f8_gradient_workspace_bytes(m, n, d)
+    need = L.efanna_f8_gradient_workspace_bytes(m, n, d, 0)
     ok = dict(dy=ONE, dtype=0, m=m, n=n, ldy=n, codes=ONE, scales=ONE, form=0, d=d, out_dtype=0, out=ONE, ldo=d, ws=ONE, size=need,
               stream=None)
     refuses(L.efanna_f8_gradient, ok,
@@ -102,6 +102,7 @@ def test_gradient(f8):
              dict(out=ODD, out_dtype=2)))
     if need:
         refuses(L.efanna_f8_gradient, ok, (dict(ws=None), dict(ws=C.c_void_p(4096 + 16)), dict(size=need - 1)), EWORKSPACE)
+    assert L.efanna_f8_gradient(*{**ok, **dict(ldy=2 ** 24)}.values()) == EUNSUPPORTED
     assert L.efanna_f8_gradient(*{**ok, **dict(n=0, ldy=0, dy=None, out=None, ws=None, size=0)}.values()) == OK
 
 
@@ -109,13 +110,15 @@ def test_workspace_sizes(f8):
     product, gradient = f8.lib().efanna_f8_product_workspace_bytes, f8.lib().efanna_f8_gradient_workspace_bytes
     for bad in ((-1, 1, 1), (1, -1, 1), (1, 1, 0), (1, 1, 65537), (2 ** 31, 1, 1)):
         assert product(*bad) == 0
-    for bad in ((-1, 1, 1), (1, -1, 1), (1, 1, 0), (1, 1, 65537), (2 ** 31, 1, 1), (1, 65537, 1)):
+    for bad in ((-1, 1, 1, 0), (1, -1, 1, 0), (1, 1, 0, 0), (1, 1, 65537, 0), (2 ** 31, 1, 1, 0), (1, 65537, 1, 0), (9999, 1, 1, 3)):
         assert gradient(*bad) == 0
     # parts of a sum are only as many as it takes to fill the GPU
     for m in (1, 40, 300, 5000, 2 ** 31 - 65537):
         for n in (1, 50, 4000, 65536):
             for d in (1, 300, 9000, 65536):
-                assert product(m, n, d) <= 256 << 20 and gradient(m, n, d) <= 256 << 20
+                assert product(m, n, d) <= 256 << 20
+                if n <= 65536:
+                    assert all(gradient(m, n, d, dtype) <= 256 << 20 for dtype in range(3))
 
 
 def test_binding_checks_types_shapes_and_devices(f8):
