@@ -78,7 +78,8 @@ template <int FORMAT> __device__ inline void sixteen_wide(i32x4 codes, float sca
 
 // ---- quantisation of rows --------------------------------------------------------------------------------
 // Sixteen lanes per block, eight coordinates each; a wave takes four blocks (their scales are one word), which are one row's
-// four, or of rows of one or two blocks four or two rows (`group` lanes a row).
+// four, or of rows of one or two blocks four or two rows (`group` lanes a row).  Rows of up to 64 coordinates take eight lanes,
+// which write the zeros after them too.
 template <class T, int FORMAT>
 __global__ __launch_bounds__(256) void f8_quantise_kernel(const T *X, u32 units, int d, long long ldx, int group, int nb, int sp,
                                                           uint8_t *codes, uint8_t *scales)
@@ -95,15 +96,15 @@ __global__ __launch_bounds__(256) void f8_quantise_kernel(const T *X, u32 units,
     for (int j = 0; j < 8; ++j) top = max(top, finite_bits(v[j]));
     top = max(top, lane_from<kSwap1>(top));
     top = max(top, lane_from<kSwap2>(top));
-    top = max(top, lane_from<kDown4>(top));
-    top = max(top, lane_from<kDown8>(top));
+    top = max(top, lane_from<kMirror8>(top));
+    if (group > 8) top = max(top, lane_from<kDown8>(top));
     const u32 b = scale_byte<FORMAT>(top);
     const float inverse = inverse_scale(b);
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] *= inverse;
-    if (block < nb)
-        *(u32x2 *)(codes + ((size_t)row * nb + block) * 128 + (lane & 15) * 8) =
-            u32x2{four_codes<FORMAT>(v[0], v[1], v[2], v[3]), four_codes<FORMAT>(v[4], v[5], v[6], v[7])};
+    uint8_t *to = codes + ((size_t)row * nb + block) * 128 + (lane & 15) * 8;
+    if (block < nb) *(u32x2 *)to = u32x2{four_codes<FORMAT>(v[0], v[1], v[2], v[3]), four_codes<FORMAT>(v[4], v[5], v[6], v[7])};
+    if (group == 8) *(u32x2 *)(to + 64) = u32x2{0, 0};
     u32 four = block < nb ? b : 0;
     if (group > 16) four |= __shfl_down(four, 16) << 8;
     if (group > 32) four |= __shfl_down(four, 32) << 16;
@@ -111,33 +112,36 @@ __global__ __launch_bounds__(256) void f8_quantise_kernel(const T *X, u32 units,
 }
 
 // ---- quantisation of a matrix by tiles of 128 x 128 ------------------------------------------------------------
-// A workgroup takes a tile: a thread holds 8 x 8 of it (rows 8 (tid / 16) on, columns 8 (tid % 16) on) in registers, all share the
+// A workgroup takes a tile: a thread holds 4 x 8 of it (rows 4 (tid / 16) on, columns 8 (tid % 16) on) in registers, all share the
 // largest magnitude, and the codes of the transpose leave through LDS as whole lines.
 template <class T, int FORMAT>
-__global__ __launch_bounds__(256) void f8_weights_kernel(const T *W, int n, int d, long long ldw, uint8_t *codes, uint8_t *scales,
+__global__ __launch_bounds__(512) void f8_weights_kernel(const T *W, int n, int d, long long ldw, uint8_t *codes, uint8_t *scales,
                                                          uint8_t *t_codes, uint8_t *t_scales)
 {
-    __shared__ u32 tops[4];
+    __shared__ u32 tops[8];
     __shared__ __align__(16) uint8_t turned[128][144];
     const int tid = threadIdx.x, nb = f8_blocks(d), sp = f8_scale_pitch(d), t_nb = f8_blocks(n), t_sp = f8_scale_pitch(n);
-    const int bx = blockIdx.x, by = blockIdx.y, r0 = by * 128 + (tid >> 4) * 8, c0 = bx * 128 + (tid & 15) * 8;
-    float v[8][8];
+    const int bx = blockIdx.x, by = blockIdx.y, r0 = by * 128 + (tid >> 4) * 4, c0 = bx * 128 + (tid & 15) * 8;
+    float v[4][8];
     u32 top = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        load_eight(W + min(r0 + i, n - 1) * ldw + c0, r0 + i < n ? d - c0 : 0, v[i]);
+    for (int i = 0; i < 4; ++i) load_eight(W + min(r0 + i, n - 1) * ldw + c0, r0 + i < n ? d - c0 : 0, v[i]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int j = 0; j < 8; ++j) top = max(top, finite_bits(v[i][j]));
-    }
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) top = max(top, (u32)__shfl_xor((int)top, o));
     if ((tid & 63) == 0) tops[tid >> 6] = top;
     __syncthreads();
-    const u32 b = scale_byte<FORMAT>(max(max(tops[0], tops[1]), max(tops[2], tops[3])));
-    const float inverse = inverse_scale(b);
-    u32 w[8][2];
+    top = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 8; ++i) top = max(top, tops[i]);
+    const u32 b = scale_byte<FORMAT>(top);
+    const float inverse = inverse_scale(b);
+    u32 w[4][2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[i][j] *= inverse;
         w[i][0] = four_codes<FORMAT>(v[i][0], v[i][1], v[i][2], v[i][3]);
@@ -152,83 +156,83 @@ __global__ __launch_bounds__(256) void f8_weights_kernel(const T *W, int n, int 
         for (int i = 1; i <= pad; ++i) s[i] = 0;
     }
     if (!t_codes) return;
-    if (tid >= 128 && bx * 128 + tid - 128 < d) {
+    if (tid >= 128 && tid < 256 && bx * 128 + tid - 128 < d) {
         uint8_t *s = t_scales + (size_t)(bx * 128 + tid - 128) * t_sp + by;
         s[0] = (uint8_t)b;
         for (int i = 1; i <= t_pad; ++i) s[i] = 0;
     }
+    // four rows' codes of a column are a word
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        u32 col[2] = {0, 0};
+    for (int h = 0; h < 2; ++h) {
+        const u32 x = __builtin_amdgcn_perm(w[1][h], w[0][h], 0x05010400), y = __builtin_amdgcn_perm(w[1][h], w[0][h], 0x07030602);
+        const u32 z = __builtin_amdgcn_perm(w[3][h], w[2][h], 0x05010400), u = __builtin_amdgcn_perm(w[3][h], w[2][h], 0x07030602);
+        const u32 col[4] = {__builtin_amdgcn_perm(z, x, 0x05040100), __builtin_amdgcn_perm(z, x, 0x07060302), __builtin_amdgcn_perm(u, y, 0x05040100),
+                            __builtin_amdgcn_perm(u, y, 0x07060302)};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) col[i >> 2] |= ((w[i][j >> 2] >> (8 * (j & 3))) & 255u) << (8 * (i & 3));
-        *(u32x2 *)&turned[(tid & 15) * 8 + j][(tid >> 4) * 8] = u32x2{col[0], col[1]};
+        for (int j = 0; j < 4; ++j) *(u32 *)&turned[(tid & 15) * 8 + 4 * h + j][(tid >> 4) * 4] = col[j];
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int c = i * 32 + (tid >> 3), part = (tid & 7) * 16;
+    for (int i = 0; i < 2; ++i) {
+        const int c = i * 64 + (tid >> 3), part = (tid & 7) * 16;
         if (bx * 128 + c < d) *(u32x4 *)(t_codes + ((size_t)(bx * 128 + c) * t_nb + by) * 128 + part) = *(const u32x4 *)&turned[c][part];
     }
 }
 
 // ---- rows by id ------------------------------------------------------------------------------------------
 // A lane per 16 bytes of an output row (4 or 8 coordinates: neighbouring lanes' stores touch), `group` lanes (a power of two)
-// per row and kRows rows per lane, so that as many chains of id, codes, store run side by side.  Codes have at most four significant
-// bits, so value * scale is exact; the factor's product is rounded to float32 and then once to the output's type.
-constexpr int kRows = 4;
-template <class T, int FORMAT, bool PAST_CACHE>
-__global__ __launch_bounds__(256) void f8_rows_kernel(F8 t, int d, const int *ids, long long m, int group, float factor, T *out)
+// per row, or per piece of a row that a workgroup takes, and ROWS rows per lane, so that as many chains of id, codes, store run side
+// by side.  Codes have at most four significant bits, so value * scale is exact; the factor's product is rounded to float32 and
+// then once to the output's type.
+template <class T, int FORMAT, int ROWS, bool PAST_CACHE>
+__global__ __launch_bounds__(256) void f8_rows_kernel(F8 t, int d, const int *ids, long long m, int group, int pieces, float factor, T *out)
 {
     constexpr int kPer = 16 / sizeof(T);
     typedef T Piece __attribute__((ext_vector_type(kPer), aligned(sizeof(T))));
-    const int lane = threadIdx.x & (group - 1), per = 256 / group;
-    const long long first = (long long)blockIdx.x * (per * kRows) + threadIdx.x / group;
-    int id[kRows];
+    const int per = 256 / group;
+    const u32 rows = pieces == 1 ? blockIdx.x : blockIdx.x / pieces;
+    const int p = (int)(blockIdx.x - rows * pieces) * group + (threadIdx.x & (group - 1));
+    const long long first = (long long)rows * (per * ROWS) + threadIdx.x / group;
+    if (p * kPer >= d) return;
+    u32 word[ROWS][2], b[ROWS];
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
+    for (int i = 0; i < ROWS; ++i) {
         const long long row = min(first + (long long)i * per, m - 1);
-        id[i] = ids ? ids[row] : (int)row;
+        const int id = ids ? ids[row] : (int)row;
+        word[i][0] = word[i][1] = 0, b[i] = 256;                   // (an empty slot)
+        if (id >= 0 && id < t.n) {
+            const uint8_t *from = t.row(id) + p * kPer;
+            if (kPer == 4) word[i][0] = *(const u32 *)from;
+            else {
+                const u32x2 x = *(const u32x2 *)from;
+                word[i][0] = x.x, word[i][1] = x.y;
+            }
+            b[i] = t.scales[(size_t)id * t.sp + p * kPer / 128];
+        }
     }
-    for (int p = lane; p * kPer < d; p += group) {
-        u32 word[kRows][2], b[kRows];
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            word[i][0] = word[i][1] = 0, b[i] = 256;                   // (an empty slot)
-            if (id[i] >= 0 && id[i] < t.n) {
-                const uint8_t *from = t.row(id[i]) + p * kPer;
-                if (kPer == 4) word[i][0] = *(const u32 *)from;
-                else {
-                    const u32x2 x = *(const u32x2 *)from;
-                    word[i][0] = x.x, word[i][1] = x.y;
-                }
-                b[i] = t.scales[(size_t)id[i] * t.sp + p * kPer / 128];
-            }
+    for (int i = 0; i < ROWS; ++i) {
+        const long long row = first + (long long)i * per;
+        float v[8];
+        four_values<FORMAT>(word[i][0], v);
+        if (kPer > 4) four_values<FORMAT>(word[i][1], v + 4);
+        const float scale = scale_value(b[i] & 255);
+        Piece x;
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            float y = v[j] * scale * factor;
+            if (sizeof(T) == 2) asm("" : "+v"(y));            // (a float32 number: not multiplied and rounded in one instruction)
+            x[j] = from_float<T>(b[i] > 255 ? 0.0f : y);
         }
+        if (row >= m) continue;
+        T *o = out + (size_t)row * d + p * kPer;
+        if (d - p * kPer >= kPer) {
+            if (PAST_CACHE) __builtin_nontemporal_store(x, (Piece *)o);
+            else *(Piece *)o = x;
+        } else
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            const long long row = first + (long long)i * per;
-            float v[8];
-            four_values<FORMAT>(word[i][0], v);
-            if (kPer > 4) four_values<FORMAT>(word[i][1], v + 4);
-            const float scale = scale_value(b[i] & 255);
-            Piece x;
-#pragma unroll
-            for (int j = 0; j < kPer; ++j) {
-                float y = v[j] * scale * factor;
-                if (sizeof(T) == 2) asm("" : "+v"(y));            // (a float32 number: not multiplied and rounded in one instruction)
-                x[j] = from_float<T>(b[i] > 255 ? 0.0f : y);
-            }
-            if (row >= m) continue;
-            T *o = out + (size_t)row * d + p * kPer;
-            if (d - p * kPer >= kPer) {
-                if (PAST_CACHE) __builtin_nontemporal_store(x, (Piece *)o);
-                else *(Piece *)o = x;
-            } else
-#pragma unroll
-                for (int j = 0; j < kPer; ++j)
-                    if (p * kPer + j < d) o[j] = x[j];
-        }
+            for (int j = 0; j < kPer; ++j)
+                if (p * kPer + j < d) o[j] = x[j];
     }
 }
 
@@ -369,16 +373,22 @@ __global__ __launch_bounds__(64 * WA * WB, FA * FB > 4 ? 1 : 2) void f8_product_
 #pragma unroll
     for (int i = 0; i < Tile::each_scales; ++i) at_scales[i] = row_of((wave * Tile::each_scales + i) * 64 + lane) * a.sp;
     const auto load = [&](int stage, bool with_scales) {
+        const uint8_t *from_a = codes_a + (size_t)stage * 128, *from_b = codes_b + (size_t)stage * 128;
+        asm volatile("" : "+s"(from_a), "+s"(from_b));        // (or else every load's address stays in two registers)
 #pragma unroll
         for (int i = 0; i < Tile::each; ++i) {
             const int op = wave * Tile::each + i;
-            stage_lds((op * 8 < Tile::side_a ? codes_a : codes_b) + stage * 128 + at_codes[i], &lds.codes[stage & 1][op][0], 1);
+            u32 at = at_codes[i];
+            asm volatile("" : "+v"(at));        // (an offset of 32 bits: not kept as one of 64)
+            stage_lds((op * 8 < Tile::side_a ? from_a : from_b) + at, &lds.codes[stage & 1][op][0], 1);
         }
         if (!with_scales) return;
 #pragma unroll
         for (int i = 0; i < Tile::each_scales; ++i) {
             const int op = wave * Tile::each_scales + i;
-            stage_lds((op * 64 < Tile::side_a ? scales_a : scales_b) + stage + at_scales[i], &lds.scales[(stage >> 2) & 1][op * 64], 0);
+            u32 at = at_scales[i];
+            asm volatile("" : "+v"(at));
+            stage_lds((op * 64 < Tile::side_a ? scales_a : scales_b) + stage + at, &lds.scales[(stage >> 2) & 1][op * 64], 0);
         }
     };
     f32x16 acc[FA][FB] = {};
@@ -953,7 +963,7 @@ extern "C" int efanna_f8_quantise(const void *X, int32_t dtype, int64_t n, int32
     if (n == 0) return EFANNA_OK;
     if (!X || !aligned_for(X, dtype)) return EFANNA_EINVAL;
     hipStream_t st = (hipStream_t)stream;
-    const int nb = f8_blocks(d), sp = f8_scale_pitch(d), words = sp / 4, group = nb == 1 ? 16 : nb == 2 ? 32 : 64;
+    const int nb = f8_blocks(d), sp = f8_scale_pitch(d), words = sp / 4, group = d <= 64 ? 8 : nb == 1 ? 16 : nb == 2 ? 32 : 64;
     const int64_t units = 256 / group, slice = kSliceBlocks * units / words;      // of a workgroup; rows of a launch
     for (int64_t first = 0; first < n; first += slice) {
         const int64_t here = (n - first < slice ? n - first : slice) * words;
@@ -973,7 +983,7 @@ extern "C" int efanna_f8_weights(const void *W, int32_t dtype, int32_t n, int32_
     if (n == 0) return EFANNA_OK;
     if (!W || !aligned_for(W, dtype)) return EFANNA_EINVAL;
     const dim3 grid((unsigned)f8_blocks(d), (unsigned)f8_blocks(n));
-    EF_DTYPE(dtype, T, EF_FORMAT(format, F, (f8_weights_kernel<T, F><<<grid, 256, 0, (hipStream_t)stream>>>(
+    EF_DTYPE(dtype, T, EF_FORMAT(format, F, (f8_weights_kernel<T, F><<<grid, 512, 0, (hipStream_t)stream>>>(
                                                 (const T *)W, n, d, ldw, codes, scales, t_codes, t_scales))));
     EF_HIP_CHECK(hipGetLastError());
     return EFANNA_OK;
@@ -987,21 +997,22 @@ extern "C" int efanna_f8_rows(const uint8_t *codes, const uint8_t *scales, int32
     if (!out || !aligned_for(out, dtype) || ((uintptr_t)ids & 3)) return EFANNA_EINVAL;
     hipStream_t st = (hipStream_t)stream;
     const F8 t = {codes, scales, (int)n, f8_blocks(d), f8_scale_pitch(d)};
-    const int per = dtype == EFANNA_F32 ? 4 : 8;
+    const int per = dtype == EFANNA_F32 ? 4 : 8, across = (d + per - 1) / per;      // coordinates of a lane, lanes of a row
     const bool past_cache = m * d * (16 / per) > kStreamBytes;
     int group = 1;
-    while (group < 64 && group * per < d) group <<= 1;
-    const int64_t rows = kRows * (256 / group), slice = kSliceBlocks * rows;      // rows of a workgroup, of a launch
+    while (group < 256 && group < across) group <<= 1;
+    const int pieces = (across + group - 1) / group;
+    const int each = m * pieces <= 2048 * (256 / group) ? 1 : 4;      // rows of a lane: one where four would leave CUs without work
+    const int64_t rows = each * (256 / group), slice = kSliceBlocks / pieces * rows;      // rows of a workgroup, of a launch
     for (int64_t first = 0; first < m; first += slice) {
         const int64_t here = m - first < slice ? m - first : slice;
-        const unsigned blocks = (unsigned)((here + rows - 1) / rows);
+        const unsigned blocks = (unsigned)((here + rows - 1) / rows * pieces);
         // (without ids the slice's rows are a table of their own)
         const F8 from = ids ? t : F8{codes + (size_t)first * t.nb * 128, scales + (size_t)first * t.sp, (int)(n - first), t.nb, t.sp};
         const int *slice_ids = ids ? ids + first : nullptr;
         EF_DTYPE(dtype, T, EF_FORMAT(format, F, {
-            T *to = (T *)out + (size_t)first * d;
-            if (past_cache) f8_rows_kernel<T, F, true><<<blocks, 256, 0, st>>>(from, d, slice_ids, here, group, factor, to);
-            else f8_rows_kernel<T, F, false><<<blocks, 256, 0, st>>>(from, d, slice_ids, here, group, factor, to);
+            const auto kernel = each == 1 ? f8_rows_kernel<T, F, 1, false> : past_cache ? f8_rows_kernel<T, F, 4, true> : f8_rows_kernel<T, F, 4, false>;
+            kernel<<<blocks, 256, 0, st>>>(from, d, slice_ids, here, group, pieces, factor, (T *)out + (size_t)first * d);
         }));
         EF_HIP_CHECK(hipGetLastError());
     }

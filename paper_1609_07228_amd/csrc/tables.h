@@ -61,8 +61,8 @@ __device__ inline void load_eight(const T *p, int left, float (&v)[8])
 
 // ---- lanes and LDS -------------------------------------------------------------------------------------
 // A neighbour's value by row operations (no trip through LDS): the other lane of a pair, of a pair of pairs; the lane 4 or
-// 8 further within a row of 16, around its end.
-constexpr int kSwap1 = 0xB1, kSwap2 = 0x4E, kDown4 = 0x120 + 12, kDown8 = 0x120 + 8;
+// 8 further within a row of 16, around its end; the eight lanes of half a row in reverse.
+constexpr int kSwap1 = 0xB1, kSwap2 = 0x4E, kDown4 = 0x120 + 12, kDown8 = 0x120 + 8, kMirror8 = 0x141;
 template <int CTRL> __device__ inline u32 lane_from(u32 x) { return (u32)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true); }
 template <int CTRL> __device__ inline float lane_from(float x) { return __uint_as_float(lane_from<CTRL>(__float_as_uint(x))); }
 
