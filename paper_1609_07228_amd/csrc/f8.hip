@@ -240,10 +240,10 @@ __global__ __launch_bounds__(256) void f8_rows_kernel(F8 t, int d, const int *id
 // Lane l of an instruction of 32 x 32 brings its part of row l % 32 of an operand: 32 bytes of a step of 64 coordinates for
 // 8-bit operands, 8 numbers of a step of 16 for bfloat16.  Which coordinates the two halves of the lanes bring does not matter as
 // long as both operands agree.  The result's lane l holds column l % 32 (of the second operand), rows 8 c + 4 (l / 32) + 0..3.
+__device__ inline i32x8 both(i32x4 a, i32x4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
 template <int FA, int FB> __device__ inline f32x16 f8_mma(i32x4 a0, i32x4 a1, int a_scale, i32x4 b0, i32x4 b1, int b_scale, f32x16 c)
 {
-    const i32x8 a = {a0.x, a0.y, a0.z, a0.w, a1.x, a1.y, a1.z, a1.w}, b = {b0.x, b0.y, b0.z, b0.w, b1.x, b1.y, b1.z, b1.w};
-    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, FA, FB, 0, a_scale, 0, b_scale);
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(both(a0, a1), both(b0, b1), c, FA, FB, 0, a_scale, 0, b_scale);
 }
 
 // Out through LDS, 32 rows of a wave's piece of 32 FA rows and 32 FB columns at a time, so that stores are whole rows of it.
@@ -467,86 +467,85 @@ __global__ __launch_bounds__(64 * WA * WB, FA * FB > 4 ? 1 : 2) void f8_product_
 }
 
 // Few rows of a (16 M at most): bound by reading b once.  A workgroup takes 16 ROWS rows of b; its waves share the blocks, and
-// their sums meet in LDS, in the waves' order.  b's codes pass through LDS by direct loads, S blocks at a time (a load brings 8
+// their sums meet in LDS, in the waves' order.  Codes of both pass through LDS by direct loads, S blocks at a time (a load brings 8
 // whole lines, ordered as in the tiles); operands are of 16 rows, lane l brings row l % 16 and the pieces l / 16 and l / 16 + 4.
-template <int ROWS, int S>
+// (16 rows against 8192 x 8192: a's operands straight from memory, rows apart in a load, 21.7 us; a byte load for each scale 17.0; so
+// 14.7.)
+template <int M, int ROWS, int S>
 struct FewLds {
-    u32 codes[S][2 * ROWS][256];
+    u32 codes[S][2 * (ROWS + M)][256];       // b's rows, then a's
 };
 template <bool WIDE, int FORMAT_A, int FORMAT_B, int M, int ROWS, int S, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void f8_product_few_kernel(F8 a, F8 b, int dtype, void *out, long long ldo)
 {
+    static_assert(S <= 2, "a stage's scales are in one word");
     extern __shared__ __align__(16) char lds_raw[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
-    FewLds<ROWS, S> *lds = (FewLds<ROWS, S> *)lds_raw + wave;
+    FewLds<M, ROWS, S> *lds = (FewLds<M, ROWS, S> *)lds_raw + wave;
     const int j0 = blockIdx.x * 16 * ROWS, left = b.n - j0;
-    const int s_lo = a.nb * wave / WAVES, s_hi = a.nb * (wave + 1) / WAVES;
+    const int groups = (a.nb + S - 1) / S, s_lo = groups * wave / WAVES * S, s_hi = min(groups * (wave + 1) / WAVES * S, a.nb);
     const uint8_t *codes_b = b.row(j0);
-    u32 at_codes[2 * ROWS];
+    u32 at_b[2 * ROWS], at_a[2 * M];
+    const int load_row = lane >> 3, load_piece = (lane & 7) ^ (load_row >> 1);      // of the rows 0 .. 7 of sixteen; 8 .. 15: the piece ^ 4
 #pragma unroll
-    for (int i = 0; i < 2 * ROWS; ++i) {
-        const int row = 8 * i + (lane >> 3);
-        at_codes[i] = (u32)min(row, left - 1) * b.nb * 128 + ((lane & 7) ^ ((row >> 1) & 7)) * 16;
-    }
-    const uint8_t *row_a[M], *scale_a[M], *scale_b[ROWS];
+    for (int i = 0; i < 2 * ROWS; ++i) at_b[i] = (u32)min(8 * i + load_row, left - 1) * b.nb * 128 + (load_piece ^ (4 * (i & 1))) * 16;
 #pragma unroll
-    for (int f = 0; f < M; ++f) {
-        const int row = min(16 * f + r, a.n - 1);
-        row_a[f] = a.row(row) + g * 16, scale_a[f] = a.scales + (size_t)row * a.sp;
-    }
+    for (int i = 0; i < 2 * M; ++i) at_a[i] = (u32)min(8 * i + load_row, a.n - 1) * a.nb * 128 + (load_piece ^ (4 * (i & 1))) * 16;
+    const uint8_t *scale_a[M], *scale_b[ROWS];
+#pragma unroll
+    for (int f = 0; f < M; ++f) scale_a[f] = a.scales + (size_t)min(16 * f + r, a.n - 1) * a.sp;
 #pragma unroll
     for (int f = 0; f < ROWS; ++f) scale_b[f] = b.scales + (size_t)(j0 + min(16 * f + r, left - 1)) * b.sp;
+    // where the lane's two pieces of its row are, within an operand of 16 rows
+    const int first = r * 128 + (g ^ ((r >> 1) & 7)) * 16, second = first ^ 64;
     f32x4 acc[M][ROWS] = {};
     for (int s0 = s_lo; s0 < s_hi; s0 += S) {
 #pragma unroll
         for (int s = 0; s < S; ++s) {
             if (S > 1 && s0 + s >= s_hi) break;
 #pragma unroll
-            for (int i = 0; i < 2 * ROWS; ++i) stage_lds(codes_b + (s0 + s) * 128 + at_codes[i], &lds->codes[s][i][0], 1);
+            for (int i = 0; i < 2 * ROWS; ++i) stage_lds(codes_b + (s0 + s) * 128 + at_b[i], &lds->codes[s][i][0], 1);
+#pragma unroll
+            for (int i = 0; i < 2 * M; ++i) stage_lds(a.codes + (s0 + s) * 128 + at_a[i], &lds->codes[s][2 * ROWS + i][0], 1);
         }
-        i32x4 y[S][M][2];
-        int sy[S][M], sx[S][ROWS];
+        u32 words_a[M], words_b[ROWS];
 #pragma unroll
-        for (int s = 0; s < S; ++s) {
-            const int at = min(s0 + s, s_hi - 1);
+        for (int f = 0; f < M; ++f) words_a[f] = *(const u32 *)(scale_a[f] + (s0 & ~3)) >> (8 * (s0 & 3));
 #pragma unroll
-            for (int f = 0; f < M; ++f) {
-                y[s][f][0] = *(const i32x4 *)(row_a[f] + at * 128), y[s][f][1] = *(const i32x4 *)(row_a[f] + at * 128 + 64);
-                sy[s][f] = scale_a[f][at];
-            }
-#pragma unroll
-            for (int f = 0; f < ROWS; ++f) sx[s][f] = scale_b[f][at];
-        }
+        for (int f = 0; f < ROWS; ++f) words_b[f] = *(const u32 *)(scale_b[f] + (s0 & ~3)) >> (8 * (s0 & 3));
         wait_loads<0>();
 #pragma unroll
         for (int s = 0; s < S; ++s) {
             if (S > 1 && s0 + s >= s_hi) break;
+            i32x4 y[M][2];
+#pragma unroll
+            for (int f = 0; f < M; ++f) {
+                const char *from = (const char *)&lds->codes[s][2 * (ROWS + f)][0];
+                y[f][0] = *(const i32x4 *)(from + first), y[f][1] = *(const i32x4 *)(from + second);
+            }
 #pragma unroll
             for (int t = 0; t < ROWS; ++t) {
-                const char *from = (const char *)&lds->codes[s][2 * t][0] + r * 128;
-                const i32x4 x0 = *(const i32x4 *)(from + ((g ^ ((r >> 1) & 7)) * 16)), x1 = *(const i32x4 *)(from + (((g + 4) ^ ((r >> 1) & 7)) * 16));
+                const char *from = (const char *)&lds->codes[s][2 * t][0];
+                const i32x4 x[2] = {*(const i32x4 *)(from + first), *(const i32x4 *)(from + second)};
+                const int x_scale = words_b[t] >> (8 * s) & 255;
                 if constexpr (WIDE) {
                     bf16x8 wide_b[2][2];
-                    sixteen_wide<FORMAT_B>(x0, scale_value(sx[s][t]), wide_b[0]);
-                    sixteen_wide<FORMAT_B>(x1, scale_value(sx[s][t]), wide_b[1]);
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) sixteen_wide<FORMAT_B>(x[q], scale_value(x_scale), wide_b[q]);
 #pragma unroll
                     for (int f = 0; f < M; ++f)
 #pragma unroll
                         for (int q = 0; q < 2; ++q) {
                             bf16x8 wide_a[2];
-                            sixteen_wide<FORMAT_A>(y[s][f][q], scale_value(sy[s][f]), wide_a);
+                            sixteen_wide<FORMAT_A>(y[f][q], scale_value(words_a[f] >> (8 * s) & 255), wide_a);
 #pragma unroll
                             for (int h = 0; h < 2; ++h) acc[f][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide_b[q][h], wide_a[h], acc[f][t], 0, 0, 0);
                         }
-                } else {
-                    const i32x8 x = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
+                } else
 #pragma unroll
-                    for (int f = 0; f < M; ++f) {
-                        const i32x4 y0 = y[s][f][0], y1 = y[s][f][1];
-                        const i32x8 ya = {y0.x, y0.y, y0.z, y0.w, y1.x, y1.y, y1.z, y1.w};
-                        acc[f][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, ya, acc[f][t], FORMAT_B, FORMAT_A, 0, sx[s][t], 0, sy[s][f]);
-                    }
-                }
+                    for (int f = 0; f < M; ++f)
+                        acc[f][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(both(x[0], x[1]), both(y[f][0], y[f][1]), acc[f][t], FORMAT_B, FORMAT_A,
+                                                                                     0, x_scale, 0, words_a[f] >> (8 * s) & 255);
             }
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // (read before it is written again)
@@ -623,7 +622,7 @@ int launch_tiles(const F8 &a, const F8 &b, int dtype, void *out, int64_t ldo, in
 template <bool WIDE, int FORMAT_A, int FORMAT_B, int M, int ROWS, int S, int WAVES>
 int launch_few(const F8 &a, const F8 &b, int dtype, void *out, int64_t ldo, hipStream_t st)
 {
-    const int stage = WAVES * (int)sizeof(FewLds<ROWS, S>), join = (WAVES - 1) * M * ROWS * 64 * 16, lds = stage > join ? stage : join;
+    const int stage = WAVES * (int)sizeof(FewLds<M, ROWS, S>), join = (WAVES - 1) * M * ROWS * 64 * 16, lds = stage > join ? stage : join;
     const int64_t blocks = ((int64_t)b.n + 16 * ROWS - 1) / (16 * ROWS);
     if (!launch_fits(blocks, 64 * WAVES)) return EFANNA_EUNSUPPORTED;
     EF_HIP_CHECK(allow_lds((const void *)f8_product_few_kernel<WIDE, FORMAT_A, FORMAT_B, M, ROWS, S, WAVES>, lds));
@@ -635,7 +634,8 @@ template <bool WIDE, int FORMAT_A, int FORMAT_B, int M>
 int launch_few_of(const F8 &a, const F8 &b, int dtype, void *out, int64_t ldo, hipStream_t st)
 {
     if (a.nb < 4) return launch_few<WIDE, FORMAT_A, FORMAT_B, M, 4, 1, 1>(a, b, dtype, out, ldo, st);
-    if (a.nb < 16) return launch_few<WIDE, FORMAT_A, FORMAT_B, M, 1, 1, 4>(a, b, dtype, out, ldo, st);
+    // (more waves for a sum where there are few rows of b; where they fill the GPU, 8192 x 8192, both take as long)
+    if (a.nb < 16 || b.n > 4096) return launch_few<WIDE, FORMAT_A, FORMAT_B, M, 1, 2, 4>(a, b, dtype, out, ldo, st);
     return launch_few<WIDE, FORMAT_A, FORMAT_B, M, 1, 2, 8>(a, b, dtype, out, ldo, st);
 }
 template <bool WIDE, int FORMAT_A, int FORMAT_B>

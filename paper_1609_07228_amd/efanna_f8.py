@@ -87,8 +87,9 @@ def _matrix(x: torch.Tensor):
 
 def _empty(n: int, d: int, form: torch.dtype, device) -> F8Table:
     nb = (d + 127) // 128
-    return F8Table(torch.empty((n, 128 * nb), dtype=form, device=device),
-                   torch.empty((n, (nb + 3) // 4 * 4), dtype=torch.uint8, device=device), d)
+    # (sizes as arguments of their own: a microsecond less than as a tuple)
+    return F8Table(torch.empty(n, 128 * nb, dtype=form, device=device),
+                   torch.empty(n, (nb + 3) // 4 * 4, dtype=torch.uint8, device=device), d)
 
 
 def efanna_f8_quantise(X: torch.Tensor, form: torch.dtype = torch.float8_e4m3fn) -> F8Table:
@@ -124,7 +125,8 @@ def efanna_f8_rows(table: F8Table, ids: torch.Tensor | None = None, factor: floa
         if ids.device != table.codes.device:
             raise ValueError("ids and table are on different devices")
     m = n if ids is None else ids.numel()
-    out = torch.empty((n, table.d) if ids is None else (*ids.shape, table.d), dtype=dtype, device=table.codes.device)
+    shape = (n,) if ids is None else ids.shape
+    out = torch.empty(*shape, table.d, dtype=dtype, device=table.codes.device)
     lib()
     _efanna._call("efanna_f8_rows", table.codes, table.codes.data_ptr(), table.scales.data_ptr(), form, n, table.d,
                   None if ids is None else ids.data_ptr(), m, float(factor), code, out.data_ptr())
