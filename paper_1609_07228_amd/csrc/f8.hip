@@ -587,25 +587,38 @@ __global__ __launch_bounds__(64 * WAVES) void f8_product_few_kernel(F8 a, F8 b, 
     else store((__bf16 *)out);
 }
 
-// How a product is cut: few rows of a, or tiles of 128 or 256 a side in as many parts of the sum as fill the GPU.
+// How a product is cut: few rows of a, or tiles of 128 or 256 a side, one of the larger or two of the smaller ones on a CU at a time,
+// and in how many parts the sum: the least of estimated times, from what the kernels were measured at.
 struct ProductShape {
     bool few;
     int side, parts;
     size_t bytes;
 };
 constexpr int kFew = 32;
-inline ProductShape product_shape(int64_t m, int64_t n, int32_t d)
+inline ProductShape product_shape(int64_t m, int64_t n, int32_t d, int32_t dtype)
 {
-    ProductShape s = {m <= kFew, 128, 1, 0};
-    if (s.few) return s;
-    const auto tiles = [&](int64_t side) { return ((m + side - 1) / side) * ((n + side - 1) / side); };
-    if (tiles(128) > 512) s.side = 256;
+    ProductShape best = {m <= kFew, 128, 1, 0};
+    if (best.few) return best;
+    // microseconds of a block of 128 coordinates; of the smaller tiles where they are a CU's only ones, too
+    const double large = dtype == EFANNA_F32 ? 3.4 : 1.8, small = dtype == EFANNA_F32 ? 2.1 : 1.2, alone = dtype == EFANNA_F32 ? 1.05 : 0.65;
     const int64_t fours = (f8_blocks(d) + 3) / 4;
-    int64_t parts = s.side == 128 ? 512 / tiles(128) : 1;
-    if (parts > fours / 2) parts = fours / 2;
-    s.parts = parts < 1 ? 1 : (int)parts;
-    s.bytes = s.parts > 1 ? align_up((size_t)s.parts * m * n * sizeof(float)) : 0;
-    return s;
+    double least = 1e300;
+    for (int side = 128; side <= 256; side += 128) {
+        const int64_t tiles = ((m + side - 1) / side) * ((n + side - 1) / side), at_once = side == 128 ? 512 : 256;
+        int64_t most = at_once / tiles;
+        if (most > fours / 2) most = fours / 2;
+        for (int64_t parts = 1; parts <= (most < 1 ? 1 : most); ++parts) {
+            const double rounds = (double)((tiles * parts + at_once - 1) / at_once), blocks = (double)((fours + parts - 1) / parts) * 4;
+            double time = rounds * (5.0 + blocks * (side == 256 ? large : tiles * parts <= 256 ? alone : small));
+            if (parts > 1) time += 3.0 + (double)parts * m * n * 8.0 / 4e6;      // written and read again
+            if (time < least) {
+                least = time;
+                best.side = side, best.parts = (int)parts;
+                best.bytes = parts > 1 ? align_up((size_t)parts * m * n * sizeof(float)) : 0;
+            }
+        }
+    }
+    return best;
 }
 template <bool WIDE, int FORMAT_A, int FORMAT_B, int FA, int FB, int WA, int WB>
 int launch_tiles(const F8 &a, const F8 &b, int dtype, void *out, int64_t ldo, int parts, float *partial, hipStream_t st)
@@ -737,17 +750,19 @@ __global__ __launch_bounds__(64 * WY * WX, 2) void f8_gradient_kernel(const Y *d
     u32 raw_scale[AHEAD][Tile::pieces_x];
     const Y *dy0 = dy + first * ldy + j0;
     const uint8_t *codes0 = x.row(first), *scales0 = x.scales + (size_t)first * x.sp;
+    const bool pieces_whole = n % 8 == 0;      // (pieces past the last column are loaded as the last one)
     const int col_y = tid % (Tile::across_y / 8) * 8, row_y = tid / (Tile::across_y / 8), rows_y = Tile::threads / (Tile::across_y / 8);
+    const int from_col = pieces_whole ? min(col_y, n - 8 - j0) : col_y;
     const int piece_x = min(c0 / 16 + tid % (Tile::across_x / 16), x.nb * 8 - 1), row_x = tid / (Tile::across_x / 16),
               rows_x = Tile::threads / (Tile::across_x / 16);
     const auto load_y = [&](int stage, int set, int i, auto inside) EF_INLINE {
         const int at = min(stage, stages - 1) * STEP, row = min(row_y + rows_y * i, rows_in - 1 - at);
         const Y *from = dy0 + at * ldy;
-        const u32 offset = (u32)row * (u32)ldy + col_y;
-        if (inside || j0 + col_y + 8 <= n) raw_y[set][i] = *(const Eight *)(from + offset);
-        else
+        const u32 offset = (u32)row * (u32)ldy;
+        if (inside || j0 + col_y + 8 <= n) raw_y[set][i] = *(const Eight *)(from + (offset + from_col));
+        else if (j0 + col_y < n)
 #pragma unroll
-            for (int k = 0; k < 8; ++k) raw_y[set][i][k] = from[(u32)row * (u32)ldy + min(col_y + k, n - 1 - j0)];        // (columns past the last one are not stored)
+            for (int k = 0; k < 8; ++k) raw_y[set][i][k] = from[offset + min(col_y + k, n - 1 - j0)];        // (columns past the last one are not stored)
     };
     const auto load_x = [&](int stage, int set, int i) EF_INLINE {
         const int at = min(stage, stages - 1) * STEP, row = min(row_x + rows_x * i, rows_in - 1 - at);
@@ -875,7 +890,7 @@ __global__ __launch_bounds__(64 * WY * WX, 2) void f8_gradient_kernel(const Y *d
         }
     };
     if (stages > 0) {
-        if (j0 + Tile::across_y <= n) run(std::true_type());
+        if (pieces_whole || j0 + Tile::across_y <= n) run(std::true_type());
         else run(std::false_type());
         meet();
     }
@@ -1019,10 +1034,10 @@ extern "C" int efanna_f8_rows(const uint8_t *codes, const uint8_t *scales, int32
     return EFANNA_OK;
 }
 
-extern "C" size_t efanna_f8_product_workspace_bytes(int64_t m, int64_t n, int32_t d)
+extern "C" size_t efanna_f8_product_workspace_bytes(int64_t m, int64_t n, int32_t d, int32_t dtype)
 {
-    if (m < 1 || m > kMaxRows || n < 1 || n > kMaxRows || d < 1 || d > EFANNA_F8_MAX_D) return 0;
-    return product_shape(m, n, d).bytes;
+    if (m < 1 || m > kMaxRows || n < 1 || n > kMaxRows || d < 1 || d > EFANNA_F8_MAX_D || !dtype_ok(dtype)) return 0;
+    return product_shape(m, n, d, dtype).bytes;
 }
 
 extern "C" int efanna_f8_product(const uint8_t *a_codes, const uint8_t *a_scales, int32_t a_format, int64_t m,
@@ -1033,7 +1048,7 @@ extern "C" int efanna_f8_product(const uint8_t *a_codes, const uint8_t *a_scales
         return EFANNA_EINVAL;
     if (m == 0 || n == 0) return EFANNA_OK;
     if (!out || !aligned_for(out, dtype)) return EFANNA_EINVAL;
-    const ProductShape sh = product_shape(m, n, d);
+    const ProductShape sh = product_shape(m, n, d, dtype);
     if (!workspace_ok(ws, ws_bytes, sh.bytes)) return EFANNA_EWORKSPACE;
     hipStream_t st = (hipStream_t)stream;
     const int nb = f8_blocks(d), sp = f8_scale_pitch(d);

@@ -36,7 +36,7 @@ def lib():
         L.efanna_f8_rows.restype = C.c_int
         L.efanna_f8_rows.argtypes = [vp, vp, i32, i64, i32, vp, i64, C.c_float, i32, vp, vp]
         L.efanna_f8_product_workspace_bytes.restype = sz
-        L.efanna_f8_product_workspace_bytes.argtypes = [i64, i64, i32]
+        L.efanna_f8_product_workspace_bytes.argtypes = [i64, i64, i32, i32]
         L.efanna_f8_product.restype = C.c_int
         L.efanna_f8_product.argtypes = [vp, vp, i32, i64, vp, vp, i32, i64, i32, i32, vp, i64, vp, sz, vp]
         L.efanna_f8_gradient_workspace_bytes.restype = sz
@@ -151,7 +151,7 @@ def efanna_f8_product(a: F8Table, b: F8Table, dtype: torch.dtype = torch.bfloat1
         raise ValueError("the tables differ in their dimension or device")
     out = _efanna._mx_out(out, (m, n), dtype, a.codes.device)
     ldo = out.stride(0) if m > 1 else max(n, 1)
-    at, size, _keep = _room(lib().efanna_f8_product_workspace_bytes(m, n, a.d), a.codes, workspace)
+    at, size, _keep = _room(lib().efanna_f8_product_workspace_bytes(m, n, a.d, code), a.codes, workspace)
     _efanna._call("efanna_f8_product", a.codes, a.codes.data_ptr(), a.scales.data_ptr(), a_form, m, b.codes.data_ptr(),
                   b.scales.data_ptr(), b_form, n, a.d, code, out.data_ptr(), ldo, at, size)
     return out

@@ -77,7 +77,7 @@ def test_rows(f8):
 def test_product(f8):
     L = f8.lib()
     m, n, d = 40, 100, 40_000
-    need = L.efanna_f8_product_workspace_bytes(m, n, d)
+    need = L.efanna_f8_product_workspace_bytes(m, n, d, 0)
     ok = dict(ac=ONE, asc=ONE, af=0, m=m, bc=ONE, bsc=ONE, bf=1, n=n, d=d, dtype=0, out=ONE, ldo=n, ws=ONE, size=need, stream=None)
     refuses(L.efanna_f8_product, ok,
             (dict(ac=None), dict(asc=None), dict(bc=None), dict(bsc=None), dict(out=None), dict(m=-1), dict(n=-1), dict(d=0),
@@ -108,7 +108,7 @@ def test_gradient(f8):
 
 def test_workspace_sizes(f8):
     product, gradient = f8.lib().efanna_f8_product_workspace_bytes, f8.lib().efanna_f8_gradient_workspace_bytes
-    for bad in ((-1, 1, 1), (1, -1, 1), (1, 1, 0), (1, 1, 65537), (2 ** 31, 1, 1)):
+    for bad in ((-1, 1, 1, 0), (1, -1, 1, 0), (1, 1, 0, 0), (1, 1, 65537, 0), (2 ** 31, 1, 1, 0), (100, 100, 60000, 3)):
         assert product(*bad) == 0
     for bad in ((-1, 1, 1, 0), (1, -1, 1, 0), (1, 1, 0, 0), (1, 1, 65537, 0), (2 ** 31, 1, 1, 0), (1, 65537, 1, 0), (9999, 1, 1, 3)):
         assert gradient(*bad) == 0
@@ -116,7 +116,7 @@ def test_workspace_sizes(f8):
     for m in (1, 40, 300, 5000, 2 ** 31 - 65537):
         for n in (1, 50, 4000, 65536):
             for d in (1, 300, 9000, 65536):
-                assert product(m, n, d) <= 256 << 20
+                assert all(product(m, n, d, dtype) <= 256 << 20 for dtype in range(3))
                 if n <= 65536:
                     assert all(gradient(m, n, d, dtype) <= 256 << 20 for dtype in range(3))
 
