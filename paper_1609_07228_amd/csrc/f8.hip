@@ -723,6 +723,23 @@ struct GradientTile {
     static constexpr int lds = (int)sizeof(Lds) > waves * turn_bytes ? (int)sizeof(Lds) : waves * turn_bytes;
 };
 
+// Eight elements from the `by`-th on (the ones after the last: anything)
+template <class Y, class Eight> __device__ inline Eight moved_down(Eight x, int by)
+{
+    constexpr int kWords = 2 * sizeof(Y);
+    typedef u32 Words __attribute__((ext_vector_type(kWords)));
+    Words w = __builtin_bit_cast(Words, x);
+    const int words = by * (int)sizeof(Y) / 4;
+#pragma unroll
+    for (int bit = 1; bit < kWords; bit *= 2)
+#pragma unroll
+        for (int k = 0; k + bit < kWords; ++k) w[k] = words & bit ? w[k + bit] : w[k];
+    if (sizeof(Y) == 2)
+#pragma unroll
+        for (int k = 0; k < kWords; ++k) w[k] = by & 1 ? w[k] >> 16 | (k + 1 < kWords ? w[k + 1] << 16 : 0) : w[k];
+    return __builtin_bit_cast(Eight, w);
+}
+
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef short i16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
@@ -748,21 +765,23 @@ __global__ __launch_bounds__(64 * WY * WX, 2) void f8_gradient_kernel(const Y *d
     Eight raw_y[AHEAD][Tile::pieces_y];
     i32x4 raw_x[AHEAD][Tile::pieces_x];
     u32 raw_scale[AHEAD][Tile::pieces_x];
-    const Y *dy0 = dy + first * ldy + j0;
+    const Y *dy0 = dy + first * ldy;
     const uint8_t *codes0 = x.row(first), *scales0 = x.scales + (size_t)first * x.sp;
-    const bool pieces_whole = n % 8 == 0;      // (pieces past the last column are loaded as the last one)
+    // (pieces past the last column, and the one that it is in, are loaded as the last eight columns and put in their place later; a
+    // matrix of fewer columns is read one by one)
+    const bool pieces_whole = n % 8 == 0;
     const int col_y = tid % (Tile::across_y / 8) * 8, row_y = tid / (Tile::across_y / 8), rows_y = Tile::threads / (Tile::across_y / 8);
-    const int from_col = pieces_whole ? min(col_y, n - 8 - j0) : col_y;
+    const int from_col = n >= 8 ? min(j0 + col_y, n - 8) : 0;      // 0 at least
     const int piece_x = min(c0 / 16 + tid % (Tile::across_x / 16), x.nb * 8 - 1), row_x = tid / (Tile::across_x / 16),
               rows_x = Tile::threads / (Tile::across_x / 16);
     const auto load_y = [&](int stage, int set, int i, auto inside) EF_INLINE {
         const int at = min(stage, stages - 1) * STEP, row = min(row_y + rows_y * i, rows_in - 1 - at);
         const Y *from = dy0 + at * ldy;
         const u32 offset = (u32)row * (u32)ldy;
-        if (inside || j0 + col_y + 8 <= n) raw_y[set][i] = *(const Eight *)(from + (offset + from_col));
-        else if (j0 + col_y < n)
+        if (inside || n >= 8) raw_y[set][i] = *(const Eight *)(from + (offset + from_col));
+        else
 #pragma unroll
-            for (int k = 0; k < 8; ++k) raw_y[set][i][k] = from[offset + min(col_y + k, n - 1 - j0)];        // (columns past the last one are not stored)
+            for (int k = 0; k < 8; ++k) raw_y[set][i][k] = from[offset + min(k, n - 1)];
     };
     const auto load_x = [&](int stage, int set, int i) EF_INLINE {
         const int at = min(stage, stages - 1) * STEP, row = min(row_x + rows_x * i, rows_in - 1 - at);
@@ -770,11 +789,13 @@ __global__ __launch_bounds__(64 * WY * WX, 2) void f8_gradient_kernel(const Y *d
         raw_scale[set][i] = *(const u32 *)(scales0 + (size_t)at * x.sp + ((u32)row * x.sp + (piece_x >> 5) * 4));
     };
     const int shift_x = 8 * ((piece_x >> 3) & 3);
-    const auto put_y = [&](int stage, int set, int buffer, int i) EF_INLINE {
+    const auto put_y = [&](int stage, int set, int buffer, int i, auto inside) EF_INLINE {
         const int piece = col_y / 8, row = row_y + rows_y * i;
         const bool live = stage * STEP + row < rows_in;
         bf16x8 part[Tile::parts];
-        Parts<Y>::split(live ? raw_y[set][i] : (Eight)(Y)0.0f, part);
+        Eight x = live ? raw_y[set][i] : (Eight)(Y)0.0f;
+        if (!inside) x = moved_down<Y>(x, n >= 8 ? j0 + col_y - from_col : 0);
+        Parts<Y>::split(x, part);
 #pragma unroll
         for (int q = 0; q < Tile::parts; ++q) *(bf16x8 *)&lds.y[buffer][q][row][((piece >> 1) ^ turn_of(row)) * 16 + (piece & 1) * 8] = part[q];
     };
@@ -844,7 +865,7 @@ __global__ __launch_bounds__(64 * WY * WX, 2) void f8_gradient_kernel(const Y *d
         };
         const auto put = [&](int stage, int set, int buffer, int i) EF_INLINE {
             if (i < Tile::pieces_x) put_x(stage, set, buffer, i);
-            else put_y(stage, set, buffer, i - Tile::pieces_x);
+            else put_y(stage, set, buffer, i - Tile::pieces_x, inside);
         };
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) load(0, 0, i);
