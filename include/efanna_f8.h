@@ -61,7 +61,7 @@ int efanna_f8_rows(const uint8_t *codes, const uint8_t *scales, int32_t format, 
  * each product cut off at 2^-14 of its group's largest: at most 2^-11 of the sum of magnitudes is lost.
  * ws     [device] 256-byte aligned, efanna_f8_product_workspace_bytes bytes; may be NULL where that is 0.
  * EFANNA_EUNSUPPORTED for what one launch does not take: 2^23 tiles of 256 x 256 and more (half a terabyte of
- * output), or up to 32 rows against 2^27 rows and more of 2048 coordinates and more. */
+ * output). */
 size_t efanna_f8_product_workspace_bytes(int64_t m, int64_t n, int32_t d, int32_t dtype);
 
 int efanna_f8_product(const uint8_t *a_codes, const uint8_t *a_scales, int32_t a_format, int64_t m,

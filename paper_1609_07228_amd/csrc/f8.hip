@@ -466,7 +466,8 @@ __global__ __launch_bounds__(64 * WA * WB, FA * FB > 4 ? 1 : 2) void f8_product_
     else store_piece<__bf16>(acc, turn, lane, (__bf16 *)out + first_row * ldo + first_col, ldo, rows_a - wa, rows_b - wb);
 }
 
-// Few rows of a (16 M at most): bound by reading b once.  A workgroup takes 16 ROWS rows of b; its waves share the blocks, and
+// Few rows of one side, here a (16 M at most): bound by reading the other, b, once; step_a and step_b lead from a result to that of the
+// next row of a and of b, one of them 1.  A workgroup takes 16 ROWS rows of b; its waves share the blocks, and
 // their sums meet in LDS, in the waves' order.  Codes of both pass through LDS by direct loads, S blocks at a time (a load brings 8
 // whole lines, ordered as in the tiles); operands are of 16 rows, lane l brings row l % 16 and the pieces l / 16 and l / 16 + 4.
 // (16 rows against 8192 x 8192: a's operands straight from memory, rows apart in a load, 21.7 us; a byte load for each scale 17.0; so
@@ -476,7 +477,7 @@ struct FewLds {
     u32 codes[S][2 * (ROWS + M)][256];       // b's rows, then a's
 };
 template <bool WIDE, int FORMAT_A, int FORMAT_B, int M, int ROWS, int S, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void f8_product_few_kernel(F8 a, F8 b, int dtype, void *out, long long ldo)
+__global__ __launch_bounds__(64 * WAVES) void f8_product_few_kernel(F8 a, F8 b, int dtype, void *out, long long step_a, long long step_b)
 {
     static_assert(S <= 2, "a stage's scales are in one word");
     extern __shared__ __align__(16) char lds_raw[];
@@ -576,10 +577,12 @@ __global__ __launch_bounds__(64 * WAVES) void f8_product_few_kernel(F8 a, F8 b, 
                 const int i = 16 * f + r, j = 16 * t + 4 * g;
                 const f32x4 v = acc[f][t];
                 if (i >= a.n || j >= left) continue;
-                T *o = to + (size_t)i * ldo + j0 + j;
-                if (left - j >= 4) *(Four *)o = Four{from_float<T>(v[0]), from_float<T>(v[1]), from_float<T>(v[2]), from_float<T>(v[3])};
+                T *o = to + i * step_a + (j0 + j) * step_b;
+                if (step_b == 1 && left - j >= 4) *(Four *)o = Four{from_float<T>(v[0]), from_float<T>(v[1]), from_float<T>(v[2]), from_float<T>(v[3])};
                 else
-                    for (int c = 0; c < left - j; ++c) o[c] = from_float<T>(v[c]);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        if (c < left - j) o[c * step_b] = from_float<T>(v[c]);
             }
     };
     if constexpr (WIDE) store((float *)out);
@@ -587,7 +590,7 @@ __global__ __launch_bounds__(64 * WAVES) void f8_product_few_kernel(F8 a, F8 b, 
     else store((__bf16 *)out);
 }
 
-// How a product is cut: few rows of a, or tiles of 128 or 256 a side, one of the larger or two of the smaller ones on a CU at a time,
+// How a product is cut: few rows of one side, or tiles of 128 or 256 a side, one of the larger or two of the smaller ones on a CU at a time,
 // and in how many parts the sum: the least of estimated times, from what the kernels were measured at.
 struct ProductShape {
     bool few;
@@ -597,7 +600,7 @@ struct ProductShape {
 constexpr int kFew = 32;
 inline ProductShape product_shape(int64_t m, int64_t n, int32_t d, int32_t dtype)
 {
-    ProductShape best = {m <= kFew, 128, 1, 0};
+    ProductShape best = {m <= kFew || n <= kFew, 128, 1, 0};
     if (best.few) return best;
     // microseconds of a block of 128 coordinates; of the smaller tiles where they are a CU's only ones, too
     const double large = dtype == EFANNA_F32 ? 3.4 : 1.8, small = dtype == EFANNA_F32 ? 2.1 : 1.2, alone = dtype == EFANNA_F32 ? 1.05 : 0.65;
@@ -633,29 +636,35 @@ int launch_tiles(const F8 &a, const F8 &b, int dtype, void *out, int64_t ldo, in
     return EFANNA_OK;
 }
 template <bool WIDE, int FORMAT_A, int FORMAT_B, int M, int ROWS, int S, int WAVES>
-int launch_few(const F8 &a, const F8 &b, int dtype, void *out, int64_t ldo, hipStream_t st)
+int launch_few(const F8 &a, const F8 &b, int dtype, void *out, int64_t step_a, int64_t step_b, hipStream_t st)
 {
     const int stage = WAVES * (int)sizeof(FewLds<M, ROWS, S>), join = (WAVES - 1) * M * ROWS * 64 * 16, lds = stage > join ? stage : join;
-    const int64_t blocks = ((int64_t)b.n + 16 * ROWS - 1) / (16 * ROWS);
-    if (!launch_fits(blocks, 64 * WAVES)) return EFANNA_EUNSUPPORTED;
     EF_HIP_CHECK(allow_lds((const void *)f8_product_few_kernel<WIDE, FORMAT_A, FORMAT_B, M, ROWS, S, WAVES>, lds));
-    f8_product_few_kernel<WIDE, FORMAT_A, FORMAT_B, M, ROWS, S, WAVES><<<(unsigned)blocks, 64 * WAVES, lds, st>>>(a, b, dtype, out, ldo);
-    EF_HIP_CHECK(hipGetLastError());
+    const int64_t slice = kSliceBlocks * 16 * ROWS * 4 / WAVES;      // rows of a launch
+    for (int64_t first = 0; first < b.n; first += slice) {
+        const int64_t here = b.n - first < slice ? b.n - first : slice;
+        const F8 from = {b.codes + (size_t)first * b.nb * 128, b.scales + (size_t)first * b.sp, (int)here, b.nb, b.sp};
+        f8_product_few_kernel<WIDE, FORMAT_A, FORMAT_B, M, ROWS, S, WAVES><<<(unsigned)((here + 16 * ROWS - 1) / (16 * ROWS)), 64 * WAVES, lds, st>>>(
+            a, from, dtype, (char *)out + first * step_b * (dtype == EFANNA_F32 ? 4 : 2), step_a, step_b);
+        EF_HIP_CHECK(hipGetLastError());
+    }
     return EFANNA_OK;
 }
 template <bool WIDE, int FORMAT_A, int FORMAT_B, int M>
-int launch_few_of(const F8 &a, const F8 &b, int dtype, void *out, int64_t ldo, hipStream_t st)
+int launch_few_of(const F8 &a, const F8 &b, int dtype, void *out, int64_t step_a, int64_t step_b, hipStream_t st)
 {
-    if (a.nb < 4) return launch_few<WIDE, FORMAT_A, FORMAT_B, M, 4, 1, 1>(a, b, dtype, out, ldo, st);
+    if (a.nb < 4) return launch_few<WIDE, FORMAT_A, FORMAT_B, M, 4, 1, 1>(a, b, dtype, out, step_a, step_b, st);
     // (more waves for a sum where there are few rows of b; where they fill the GPU, 8192 x 8192, both take as long)
-    if (a.nb < 16 || b.n > 4096) return launch_few<WIDE, FORMAT_A, FORMAT_B, M, 1, 2, 4>(a, b, dtype, out, ldo, st);
-    return launch_few<WIDE, FORMAT_A, FORMAT_B, M, 1, 2, 8>(a, b, dtype, out, ldo, st);
+    if (a.nb < 16 || b.n > 4096) return launch_few<WIDE, FORMAT_A, FORMAT_B, M, 1, 2, 4>(a, b, dtype, out, step_a, step_b, st);
+    return launch_few<WIDE, FORMAT_A, FORMAT_B, M, 1, 2, 8>(a, b, dtype, out, step_a, step_b, st);
 }
 template <bool WIDE, int FORMAT_A, int FORMAT_B>
 int launch_product(const F8 &a, const F8 &b, int dtype, void *out, int64_t ldo, const ProductShape &sh, float *partial, hipStream_t st)
 {
-    if (sh.few) return a.n <= 16 ? launch_few_of<WIDE, FORMAT_A, FORMAT_B, 1>(a, b, dtype, out, ldo, st)
-                                 : launch_few_of<WIDE, FORMAT_A, FORMAT_B, 2>(a, b, dtype, out, ldo, st);
+    if (sh.few && a.n <= kFew) return a.n <= 16 ? launch_few_of<WIDE, FORMAT_A, FORMAT_B, 1>(a, b, dtype, out, ldo, 1, st)
+                                                : launch_few_of<WIDE, FORMAT_A, FORMAT_B, 2>(a, b, dtype, out, ldo, 1, st);
+    if (sh.few) return b.n <= 16 ? launch_few_of<WIDE, FORMAT_B, FORMAT_A, 1>(b, a, dtype, out, 1, ldo, st)
+                                 : launch_few_of<WIDE, FORMAT_B, FORMAT_A, 2>(b, a, dtype, out, 1, ldo, st);
     return sh.side == 256 ? launch_tiles<WIDE, FORMAT_A, FORMAT_B, 4, 2, 2, 4>(a, b, dtype, out, ldo, sh.parts, partial, st)
                           : launch_tiles<WIDE, FORMAT_A, FORMAT_B, 2, 2, 2, 2>(a, b, dtype, out, ldo, sh.parts, partial, st);
 }
