@@ -79,7 +79,8 @@ template <int FORMAT> __device__ inline void sixteen_wide(i32x4 codes, float sca
 // ---- quantisation of rows --------------------------------------------------------------------------------
 // Sixteen lanes per block, eight coordinates each; a wave takes four blocks (their scales are one word), which are one row's
 // four, or of rows of one or two blocks four or two rows (`group` lanes a row).  Rows of up to 64 coordinates take eight lanes,
-// which write the zeros after them too.
+// which write the zeros after them too.  Bound: HBM (65 536 x 4096 bfloat16, 809 MB: 147 us, 5.5 TB/s), instructions for short rows
+// (200 003 x 50 half precision: 13.0 us; with sixteen lanes a row 17.7).
 template <class T, int FORMAT>
 __global__ __launch_bounds__(256) void f8_quantise_kernel(const T *X, u32 units, int d, long long ldx, int group, int nb, int sp,
                                                           uint8_t *codes, uint8_t *scales)
@@ -113,7 +114,9 @@ __global__ __launch_bounds__(256) void f8_quantise_kernel(const T *X, u32 units,
 
 // ---- quantisation of a matrix by tiles of 128 x 128 ------------------------------------------------------------
 // A workgroup takes a tile: a thread holds 4 x 8 of it (rows 4 (tid / 16) on, columns 8 (tid % 16) on) in registers, all share the
-// largest magnitude, and the codes of the transpose leave through LDS as whole lines.
+// largest magnitude, and the codes of the transpose leave through LDS as whole lines.  Bound: HBM (8192^2 float32 to both tables,
+// 407 MB: 69 us, 5.9 TB/s); a few tiles (128 x 960: 5.1 us) the chain of loads, maximum and stores, which is why 512 threads share a
+// tile (256 take 8.1).
 template <class T, int FORMAT>
 __global__ __launch_bounds__(512) void f8_weights_kernel(const T *W, int n, int d, long long ldw, uint8_t *codes, uint8_t *scales,
                                                          uint8_t *t_codes, uint8_t *t_scales)
@@ -183,7 +186,8 @@ __global__ __launch_bounds__(512) void f8_weights_kernel(const T *W, int n, int 
 // A lane per 16 bytes of an output row (4 or 8 coordinates: neighbouring lanes' stores touch), `group` lanes (a power of two)
 // per row, or per piece of a row that a workgroup takes, and ROWS rows per lane, so that as many chains of id, codes, store run side
 // by side.  Codes have at most four significant bits, so value * scale is exact; the factor's product is rounded to float32 and
-// then once to the output's type.
+// then once to the output's type.  Bound: HBM writes (65 536 x 4096 to bfloat16, 806 MB: 136 us, 5.9 TB/s; a wave per row that goes
+// through its pieces took 160).
 template <class T, int FORMAT, int ROWS, bool PAST_CACHE>
 __global__ __launch_bounds__(256) void f8_rows_kernel(F8 t, int d, const int *ids, long long m, int group, int pieces, float factor, T *out)
 {
@@ -296,7 +300,7 @@ __device__ inline Place place_of(u32 id, int tiles_y, int tiles_x, int parts)
     return {strip * 8 + in % high, in / high, part};
 }
 
-// Sums of the parts, in their order: a lane per result, eight loads on their way.
+// Sums of the parts, in their order: a lane per result, eight loads on their way (125 parts of 128 x 960: 10.6 us, 5.8 TB/s).
 template <class T>
 __global__ __launch_bounds__(256) void f8_join_kernel(const float *partial, int parts, u32 rows, u32 columns, T *out, long long ldo)
 {
@@ -333,8 +337,14 @@ int launch_join(const float *partial, int parts, int64_t rows, int64_t columns, 
 // WA x WB waves share a tile of a's rows by b's rows, FA x FB instructions of 32 x 32 each.  A stage is a block of both, whole
 // lines of 128 bytes, and every fourth one brings the scales of four; while one is computed the next is on its way into LDS.  A
 // load of codes brings 8 rows; the 16-byte pieces of row r lie in the order p ^ (r / 2) % 8, so that pieces p of 16 rows,
-// which are read together, are in different ones of the 64 banks.  WIDE: codes are turned into bfloat16 numbers on their way from
-// LDS, scales applied, so that products and sums are those of float32.
+// which are read together, are in different ones of the 64 banks.
+// The 8-bit matrix instructions multiply exactly, but cut each of eight products that they add first at 2^-14 of the largest of
+// them (a product of 2^3 next to one of 2^17 is kept, one of 2^2 is not), which is below half a step of a 16-bit result wherever it is
+// not much smaller than its terms, and too much for one of float32.  WIDE, for those: codes are turned into bfloat16 numbers on their way
+// from LDS, scales applied, and the bfloat16 instructions' sums are float32's (8192^3: 0.86 ms instead of 0.45).
+// Bound: power.  8192^3 takes 0.45 ms, 2.4 PFLOP/s, at 1.87 GHz with the matrix units busy for 0.59 of the time (a library product of
+// this size: 0.405); the same instructions on zeros run at 2.33 GHz, 0.37 ms.  Reading operands a piece of work ahead, as the gradient's
+// kernel does, spills registers here (0.6 ms), and loads asked for before, between or after the reads make no difference.
 template <int FA, int FB, int WA, int WB>
 struct ProductTile {
     static constexpr int waves = WA * WB, side_a = 32 * FA * WA, side_b = 32 * FB * WB, sides = side_a + side_b;
@@ -470,8 +480,8 @@ __global__ __launch_bounds__(64 * WA * WB, FA * FB > 4 ? 1 : 2) void f8_product_
 // next row of a and of b, one of them 1.  A workgroup takes 16 ROWS rows of b; its waves share the blocks, and
 // their sums meet in LDS, in the waves' order.  Codes of both pass through LDS by direct loads, S blocks at a time (a load brings 8
 // whole lines, ordered as in the tiles); operands are of 16 rows, lane l brings row l % 16 and the pieces l / 16 and l / 16 + 4.
-// (16 rows against 8192 x 8192: a's operands straight from memory, rows apart in a load, 21.7 us; a byte load for each scale 17.0; so
-// 14.7.)
+// (16 rows against 8192 x 8192: 12 us, 5.7 TB/s; with a's operands straight from memory, rows apart in a load, 19; one row against
+// 10^6 x 128: 19 us.)
 template <int M, int ROWS, int S>
 struct FewLds {
     u32 codes[S][2 * (ROWS + M)][256];       // b's rows, then a's
@@ -591,7 +601,9 @@ __global__ __launch_bounds__(64 * WAVES) void f8_product_few_kernel(F8 a, F8 b, 
 }
 
 // How a product is cut: few rows of one side, or tiles of 128 or 256 a side, one of the larger or two of the smaller ones on a CU at a time,
-// and in how many parts the sum: the least of estimated times, from what the kernels were measured at.
+// and in how many parts the sum: the least of estimated times, from what the kernels were measured at.  (1024 x 4096 x 4096 to bfloat16:
+// 34 us in two parts of smaller tiles, 26 in one; 64 x 8192 x 8192 23 us in 8 parts, 20 in 4; 32 rows as few 15.7 us, in tiles 18.6.
+// 10^6 x 1 x 128: 21 us as few rows, in tiles 68.)
 struct ProductShape {
     bool few;
     int side, parts;
@@ -713,7 +725,11 @@ __device__ inline bf16x8 without_infinities(bf16x8 x)
 // WY x WX waves share a tile of dY's columns by the table's, FY x FX instructions of 32 x 32 x 16 each, and STEP rows are a
 // stage.  Both operands are wanted by columns and lie in rows: rows go to LDS as bfloat16 numbers (dY in its parts, codes with
 // their scale applied, through registers, where AHEAD stages are on their way) and come back through transposing reads, of which a
-// lane gets four rows' values of its column.  A row's pieces of 16 columns (32 bytes) lie in the order u ^ turn_of(row), so that the
+// lane gets four rows' values of its column.
+// Bound: power and the vector and LDS work between matrix instructions.  16 384 rows, 4096 x 4096, bfloat16: 0.476 ms, 1.15 PFLOP/s, at
+// 1.84 GHz with the matrix units busy for 0.57 (zeros: 2.2 GHz, 0.41 ms; a library product of two bfloat16 matrices: 0.37); without
+// putting stages down 0.39, without reading operands either 0.31.  Rows of dY straight into LDS, three stages of them or 64 rows a stage
+// were no faster; waves of 128 x 128 spill.  A row's pieces of 16 columns (32 bytes) lie in the order u ^ turn_of(row), so that the
 // eight rows that a read touches are in different banks.
 __device__ inline int turn_of(int row) { return 2 * (row & 3) + ((row >> 2) & 1); }
 
@@ -865,7 +881,6 @@ __global__ __launch_bounds__(64 * WY * WX, 2) void f8_gradient_kernel(const Y *d
         asm volatile("" ::: "memory");
     };
     static_assert(kUnits % 2 == 0 && AHEAD <= 2, "operands and sets alternate");
-    static_assert(kUnits % 2 == 0 && AHEAD <= 2, "operands and sets alternate");
     constexpr int kPieces = Tile::pieces_x + Tile::pieces_y;
     const auto run = [&](auto inside) EF_INLINE {      // INSIDE: whole pieces of dY, without a look at where its rows end
         const auto load = [&](int stage, int set, int i) EF_INLINE {
@@ -934,7 +949,8 @@ __global__ __launch_bounds__(64 * WY * WX, 2) void f8_gradient_kernel(const Y *d
 
 // How a gradient is cut: which tile, and in how many parts the sum.  The larger tiles move half as much per operation, one at a time
 // on a CU; the wide one is for few columns of dY; two of the small ones run on a CU and leave half as many sums to be joined.  The
-// choice is the least of estimated times, from what the kernels were measured at.
+// choice is the least of estimated times, from what the kernels were measured at.  (100 000 x 128 x 960 in float32: small tiles in 64 parts
+// 110 us and 6 for their sums, wide ones in 125 parts 78 and 11; 1000 x 50 x 300: small tiles in 16 parts 7.8 and 2, in 4 parts 12.)
 constexpr int kStep = 32;
 enum GradientKind { kSquare, kWide, kSmall };
 struct GradientShape {

@@ -134,7 +134,7 @@ def efanna_f8_rows(table: F8Table, ids: torch.Tensor | None = None, factor: floa
 
 
 def _room(need: int, on: torch.Tensor, given: torch.Tensor | None):
-    """(address, bytes) of the workspace: `given`, or else a new one where one is needed."""
+    """(address, bytes, tensor) of the workspace: `given`, or else a new one where one is needed."""
     if given is None and need == 0:
         return None, 0, None
     ws = _efanna._workspace(need, on, given)
