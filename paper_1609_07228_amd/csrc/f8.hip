@@ -600,6 +600,20 @@ __global__ __launch_bounds__(64 * WAVES) void f8_product_few_kernel(F8 a, F8 b, 
     else store((__bf16 *)out);
 }
 
+// Calls try_(parts, units of a part) for numbers of parts that a sum of `units` can be cut in: at most `fill`, or `most` where that is
+// less, one at least.
+template <class F> inline void least_of_parts(int64_t fill, int64_t units, int64_t most, F try_)
+{
+    if (fill < most) most = fill;
+    if (most < 1) most = 1;
+    for (int64_t p = 1;; p = p < 4 ? p + 1 : p * 5 / 4) {
+        if (p > most) p = most;
+        const int64_t each = units > p ? (units + p - 1) / p : 1;
+        try_(units > 0 ? (units + each - 1) / each : 1, each);
+        if (p == most) return;
+    }
+}
+
 // How a product is cut: few rows of one side, or tiles of 128 or 256 a side, one of the larger or two of the smaller ones on a CU at a time,
 // and in how many parts the sum: the least of estimated times, from what the kernels were measured at.  (1024 x 4096 x 4096 to bfloat16:
 // 34 us in two parts of smaller tiles, 26 in one; 64 x 8192 x 8192 23 us in 8 parts, 20 in 4; 32 rows as few 15.7 us, in tiles 18.6.
@@ -620,18 +634,16 @@ inline ProductShape product_shape(int64_t m, int64_t n, int32_t d, int32_t dtype
     double least = 1e300;
     for (int side = 128; side <= 256; side += 128) {
         const int64_t tiles = ((m + side - 1) / side) * ((n + side - 1) / side), at_once = side == 128 ? 512 : 256;
-        int64_t most = at_once / tiles;
-        if (most > fours / 2) most = fours / 2;
-        for (int64_t parts = 1; parts <= (most < 1 ? 1 : most); ++parts) {
-            const double rounds = (double)((tiles * parts + at_once - 1) / at_once), blocks = (double)((fours + parts - 1) / parts) * 4;
-            double time = rounds * (5.0 + blocks * (side == 256 ? large : tiles * parts <= 256 ? alone : small));
+        least_of_parts(at_once / tiles, fours, fours / 2, [&](int64_t parts, int64_t each) {
+            const double rounds = (double)((tiles * parts + at_once - 1) / at_once);
+            double time = rounds * (5.0 + (double)each * 4 * (side == 256 ? large : tiles * parts <= 256 ? alone : small));
             if (parts > 1) time += 3.0 + (double)parts * m * n * 8.0 / 4e6;      // written and read again
             if (time < least) {
                 least = time;
                 best.side = side, best.parts = (int)parts;
                 best.bytes = parts > 1 ? align_up((size_t)parts * m * n * sizeof(float)) : 0;
             }
-        }
+        });
     }
     return best;
 }
@@ -731,7 +743,8 @@ __device__ inline bf16x8 without_infinities(bf16x8 x)
 // putting stages down 0.39, without reading operands either 0.31.  Rows of dY straight into LDS, three stages of them or 64 rows a stage
 // were no faster; waves of 128 x 128 spill.  A row's pieces of 16 columns (32 bytes) lie in the order u ^ turn_of(row), so that the
 // eight rows that a read touches are in different banks.
-__device__ inline int turn_of(int row) { return 2 * (row & 3) + ((row >> 2) & 1); }
+// (rows of 64 columns are four pieces: two of the eight rows in the same banks)
+template <int ACROSS> __device__ inline int turn_of(int row) { return (2 * (row & 3) + ((row >> 2) & 1)) & (ACROSS / 16 - 1); }
 
 // (a closure that is called twice and not inlined keeps what it captures, the accumulators too, in memory)
 #define EF_INLINE __attribute__((always_inline))
@@ -822,7 +835,7 @@ __global__ __launch_bounds__(64 * WY * WX, 2) void f8_gradient_kernel(const Y *d
         if (!inside) x = moved_down<Y>(x, n >= 8 ? j0 + col_y - from_col : 0);
         Parts<Y>::split(x, part);
 #pragma unroll
-        for (int q = 0; q < Tile::parts; ++q) *(bf16x8 *)&lds.y[buffer][q][row][((piece >> 1) ^ turn_of(row)) * 16 + (piece & 1) * 8] = part[q];
+        for (int q = 0; q < Tile::parts; ++q) *(bf16x8 *)&lds.y[buffer][q][row][((piece >> 1) ^ turn_of<Tile::across_y>(row)) * 16 + (piece & 1) * 8] = part[q];
     };
     const auto put_x = [&](int stage, int set, int buffer, int i) EF_INLINE {
         const int piece = tid % (Tile::across_x / 16), row = row_x + rows_x * i;
@@ -835,7 +848,7 @@ __global__ __launch_bounds__(64 * WY * WX, 2) void f8_gradient_kernel(const Y *d
         const bool swap = tid & 4;
         const i32x4 c = live ? raw_x[set][i] : i32x4{0, 0, 0, 0};
         sixteen_wide<FORMAT>(swap ? i32x4{c.z, c.w, c.x, c.y} : c, scale_value(live ? scale : 127), wide);
-        __bf16 *to = &lds.x[buffer][row][(piece ^ turn_of(row)) * 16 + (swap ? 8 : 0)];
+        __bf16 *to = &lds.x[buffer][row][(piece ^ turn_of<Tile::across_x>(row)) * 16 + (swap ? 8 : 0)];
         *(bf16x8 *)to = wide[0];
         *(bf16x8 *)(to + (swap ? -8 : 8)) = wide[1];
     };
@@ -846,9 +859,9 @@ __global__ __launch_bounds__(64 * WY * WX, 2) void f8_gradient_kernel(const Y *d
     const int row = 4 * half + ((lane >> 2) & 3), group = (lane >> 4) & 1, quarter = (lane & 3) * 4;
     int at_y[FY], at_x[FX];
 #pragma unroll
-    for (int f = 0; f < FY; ++f) at_y[f] = row * Tile::across_y + (((wy * FY + f) * 2 + group) ^ turn_of(row)) * 16 + quarter;
+    for (int f = 0; f < FY; ++f) at_y[f] = row * Tile::across_y + (((wy * FY + f) * 2 + group) ^ turn_of<Tile::across_y>(row)) * 16 + quarter;
 #pragma unroll
-    for (int f = 0; f < FX; ++f) at_x[f] = row * Tile::across_x + (((wx * FX + f) * 2 + group) ^ turn_of(row)) * 16 + quarter;
+    for (int f = 0; f < FX; ++f) at_x[f] = row * Tile::across_x + (((wx * FX + f) * 2 + group) ^ turn_of<Tile::across_x>(row)) * 16 + quarter;
     const auto columns = [](const __bf16 *from, int pitch) {      // sixteen rows' values of the lane's column, as an operand
         const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)from);
         const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(from + 8 * pitch));
@@ -948,11 +961,11 @@ __global__ __launch_bounds__(64 * WY * WX, 2) void f8_gradient_kernel(const Y *d
 }
 
 // How a gradient is cut: which tile, and in how many parts the sum.  The larger tiles move half as much per operation, one at a time
-// on a CU; the wide one is for few columns of dY; two of the small ones run on a CU and leave half as many sums to be joined.  The
-// choice is the least of estimated times, from what the kernels were measured at.  (100 000 x 128 x 960 in float32: small tiles in 64 parts
-// 110 us and 6 for their sums, wide ones in 125 parts 78 and 11; 1000 x 50 x 300: small tiles in 16 parts 7.8 and 2, in 4 parts 12.)
-constexpr int kStep = 32;
-enum GradientKind { kSquare, kWide, kSmall };
+// on a CU; the wide one is for few columns of dY; two of the small ones run on a CU and leave half as many sums to be joined, and the
+// narrow one is for 64 columns and fewer.  The choice is the least of estimated times, from what the kernels were measured at.
+// (100 000 x 128 x 960 in float32: small tiles in 64 parts 110 us and 6 for their sums, wide ones in 125 parts 78 and 11; 1000 x 50 x 300:
+// small tiles in 16 parts 7.8 and 2, in 4 parts 12; 8410 x 56 x 4585 in 14 parts: small tiles 24.0, narrow ones 18.6.)
+enum GradientKind { kSquare, kWide, kSmall, kNarrow };
 struct GradientShape {
     int kind, parts;
     size_t bytes;
@@ -961,27 +974,26 @@ inline GradientShape gradient_shape(int64_t m, int32_t n, int32_t d, int32_t dty
 {
     struct Kind {
         int y, x, at_once;             // sides, workgroups that run at once
-        double stage[3];               // microseconds, by parts of an element of dY
+        double stage[3];               // microseconds of 32 rows, by parts of an element of dY
     };
-    static const Kind kinds[3] = {{256, 256, 256, {0.95, 1.75, 3.2}}, {128, 512, 256, {1.05, 1.9, 2.9}}, {128, 128, 512, {0.75, 1.3, 2.1}}};
+    static const Kind kinds[4] = {{256, 256, 256, {0.95, 1.75, 3.2}}, {128, 512, 256, {1.05, 1.9, 2.9}}, {128, 128, 512, {0.7, 1.3, 2.1}},
+                                  {64, 128, 512, {0.5, 0.9, 1.45}}};
     const int p = dtype == EFANNA_F32 ? 2 : dtype == EFANNA_F16 ? 1 : 0;
-    const int64_t stages = (m + kStep - 1) / kStep;
+    const int64_t stages = (m + 31) / 32;
     GradientShape best = {kSmall, 1, 0};
     double least = 1e300;
-    for (int k = 0; k < 3; ++k) {
+    for (int k = 0; k < 4; ++k) {
         const int64_t tiles = (int64_t)((n + kinds[k].y - 1) / kinds[k].y) * ((d + kinds[k].x - 1) / kinds[k].x);
-        int64_t most = kinds[k].at_once / tiles;
-        if (most > stages / 2) most = stages / 2;
-        for (int64_t parts = 1; parts <= (most < 1 ? 1 : most); ++parts) {
+        least_of_parts(kinds[k].at_once / tiles, stages, stages / 2, [&](int64_t parts, int64_t each) {
             const int64_t rounds = (tiles * parts + kinds[k].at_once - 1) / kinds[k].at_once;
-            const double alone = 2 * tiles * parts <= kinds[k].at_once && k == kSmall ? 0.65 : 1.0;      // a CU's only one
-            double time = rounds * (6.0 + (double)((stages + parts - 1) / parts) * kinds[k].stage[p] * alone);
+            const double alone = 2 * tiles * parts <= kinds[k].at_once && k >= kSmall ? 0.65 : 1.0;      // a CU's only one
+            double time = rounds * (6.0 + (double)each * kinds[k].stage[p] * alone);
             if (parts > 1) time += 3.0 + (double)parts * n * d * 8.0 / 4e6;      // written and read again
             if (time < least) {
                 least = time;
                 best = {k, (int)parts, parts > 1 ? align_up((size_t)parts * n * d * sizeof(float)) : 0};
             }
-        }
+        });
     }
     return best;
 }
@@ -1130,10 +1142,12 @@ extern "C" int efanna_f8_gradient(const void *dY, int32_t dtype, int64_t m, int3
     const F8 x = {codes, scales, (int)m, f8_blocks(d), f8_scale_pitch(d)};
     int rc = EFANNA_OK;
     EF_DTYPE(dtype, Y, EF_FORMAT(format, F, {
-        constexpr int ahead = Parts<Y>::count == 3 ? 1 : 2;
-        const auto run = sh.kind == kSquare ? launch_gradient<Y, F, 4, 2, 2, 4, kStep, ahead>
-                         : sh.kind == kWide ? launch_gradient<Y, F, 4, 2, 1, 8, kStep, ahead>
-                                            : launch_gradient<Y, F, 2, 2, 2, 2, kStep, 2>;
+        // (stages of 64 rows where dY is one part: 16 384 x 1024 x 1024 51 us instead of 56; the square tiles' would spill)
+        constexpr int ahead = Parts<Y>::count == 3 ? 1 : 2, step = Parts<Y>::count == 1 ? 64 : 32, few_ahead = step == 64 ? 1 : 2;
+        const auto run = sh.kind == kSquare ? launch_gradient<Y, F, 4, 2, 2, 4, 32, ahead>
+                         : sh.kind == kWide ? launch_gradient<Y, F, 4, 2, 1, 8, 32, ahead>
+                         : sh.kind == kSmall ? launch_gradient<Y, F, 2, 2, 2, 2, step, few_ahead>
+                                             : launch_gradient<Y, F, 1, 2, 2, 2, step, few_ahead>;
         rc = run((const Y *)dY, ldy, m, n, x, d, out_dtype, out, ldo, sh.parts, (float *)ws, st);
     }));
     if (rc != EFANNA_OK || sh.parts == 1) return rc;
