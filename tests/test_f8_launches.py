@@ -2,6 +2,7 @@
 are taken by a stand-in that hands every launch to the test.  A launch takes fewer than 2^32 threads along an axis, and the launches
 of a call together have to take every row once."""
 import json
+import re
 import subprocess
 import sys
 
@@ -20,7 +21,7 @@ class Table(C.Structure):
     _fields_ = [("codes", C.c_uint64), ("scales", C.c_uint64), ("n", C.c_int), ("nb", C.c_int), ("sp", C.c_int)]
 def on_launch(f, gx, gy, gz, bx, by, bz, args):
     name = re.search(r"(f8_[a-z_]+_kernel)", names[f].decode()).group(1)
-    one = dict(kernel=name, grid=[gx, gy, gz], block=[bx, by, bz])
+    one = dict(kernel=name, grid=[gx, gy, gz], block=[bx, by, bz], symbol=names[f].decode())
     if name == "f8_quantise_kernel":
         one.update(x=value(args, 0, C.c_uint64), n=value(args, 1, C.c_uint32), group=value(args, 4, C.c_int),
                    codes=value(args, 7, C.c_uint64), scales=value(args, 8, C.c_uint64))
@@ -165,3 +166,31 @@ def test_gradients_and_weights_of_all_sizes(launches, n, d):
         assert [one["kernel"] for one in got["launches"]] in (["f8_gradient_kernel"], ["f8_gradient_kernel", "f8_join_kernel"])
     got, = launches([("efanna_f8_weights", (BASE, 1, n, d, d, 1, BASE, BASE, BASE, BASE, None))])
     assert got["status"] == 0 and got["launches"][0]["grid"] == [(d + 127) // 128, (n + 127) // 128, 1]
+
+
+def numbers(symbol):
+    """A kernel's template arguments that are numbers."""
+    return tuple(int(v) for v in re.findall(r"L[ib](\d+)E", symbol))
+
+
+def test_every_kernel_runs_in_the_tests_of_results(launches):
+    """The shapes that results are tested with reach every variant of every kernel, alone and in parts."""
+    import test_gpu_f8 as small
+    import test_gpu_f8_tiles as large
+    gradients, products = {}, {}
+    calls = [("efanna_f8_gradient", (BASE, t, m, n, n, BASE, BASE, 0, d, 0, OUT, d, BASE, 1 << 40, None))
+             for t in range(3) for m, n, d in small.GRADIENT_SHAPES + large.GRADIENT_SHAPES]
+    for (_, args), got in zip(calls, launches(calls)):
+        gradients.setdefault(args[1], set()).add((numbers(got["launches"][0]["symbol"])[1:5], len(got["launches"])))
+    for t in range(3):
+        assert {tile for tile, _ in gradients[t]} == {(4, 2, 2, 4), (4, 2, 1, 8), (2, 2, 2, 2), (1, 2, 2, 2)}, t
+        assert {parts for _, parts in gradients[t]} == {1, 2}
+    calls = [("efanna_f8_product", (BASE, BASE, 0, m, BASE, BASE, 0, n, d, t, OUT, n, BASE, 1 << 40, None))
+             for t in (0, 2) for m, n, d in small.SHAPES + large.PRODUCT_SHAPES]
+    for (_, args), got in zip(calls, launches(calls)):
+        one = got["launches"][0]
+        products.setdefault(args[9], set()).add((one["kernel"], numbers(one["symbol"])[3:], len(got["launches"])))
+    for t in (0, 2):
+        few = {v for k, v, _ in products[t] if k == "f8_product_few_kernel"}
+        assert few == {(m, *rest) for m in (1, 2) for rest in ((4, 1, 1), (1, 2, 4), (1, 2, 8))}, t
+        assert {(v, parts) for k, v, parts in products[t] if k == "f8_product_tile_kernel"} == {(tile, parts) for tile in ((4, 2, 2, 4), (2, 2, 2, 2)) for parts in (1, 2)}, t
