@@ -19,7 +19,8 @@ from paper_1609_07228_amd import efanna, efanna_f8, synth  # noqa: E402
 
 
 class F8Linear(torch.autograd.Function):
-    """x w^T with operands in 8 bits (E4M3 forward, E5M2 for the gradient on its way back); sums in float32."""
+    """x w^T with operands in 8 bits (E4M3 forward, E5M2 for the gradient on its way back); sums in float32.  Gradients have no
+    gradients of their own (asking for them is an error)."""
 
     @staticmethod
     def forward(ctx, x, w):
@@ -30,6 +31,7 @@ class F8Linear(torch.autograd.Function):
         return efanna_f8.efanna_f8_product(kept, table, dtype=x.dtype)
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
         codes, scales, t_codes, t_scales = ctx.saved_tensors
         n, d = ctx.shape

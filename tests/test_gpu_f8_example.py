@@ -56,6 +56,43 @@ def test_only_what_is_asked_for(example):
     assert torch.equal(w.grad, torch.full((6, 40), 9.0, device="cuda")) and x.grad is None
 
 
+def test_gradients_of_gradients_are_refused(example):
+    x = torch.ones((9, 40), device="cuda", requires_grad=True)
+    w = torch.ones((6, 40), device="cuda", requires_grad=True)
+    dx, = torch.autograd.grad(example.F8Linear.apply(x, w).square().sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError):
+        dx.sum().backward()
+
+
+def test_a_captured_step_with_its_backward_pass(example):
+    """Replayed several times with eager work between; inputs change in place."""
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    x = torch.randn((600, 200), generator=gen, device="cuda").requires_grad_()
+    w = torch.randn((70, 200), generator=gen, device="cuda").requires_grad_()
+
+    def step(x, w):
+        y = example.F8Linear.apply(x, w)
+        return (y.detach(), *torch.autograd.grad(y, (x, w), y.detach().sign()))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(x, w)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        kept = step(x, w)
+    for _ in range(4):
+        with torch.no_grad():
+            x.copy_(torch.randn(x.shape, generator=gen, device="cuda"))
+            w.copy_(torch.randn(w.shape, generator=gen, device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in kept]
+        want = step(x.detach().clone().requires_grad_(), w.detach().clone().requires_grad_())
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def test_example_runs_as_a_whole(example):
     got = example.run("gmm10k_d32", 3000, 16, 5, 200)
     assert set(got) == {"before", "after"} and all(0.0 <= v <= 1.0 for v in got.values())
