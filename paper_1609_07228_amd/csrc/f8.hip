@@ -738,12 +738,12 @@ __device__ inline bf16x8 without_infinities(bf16x8 x)
 // stage.  Both operands are wanted by columns and lie in rows: rows go to LDS as bfloat16 numbers (dY in its parts, codes with
 // their scale applied, through registers, where AHEAD stages are on their way) and come back through transposing reads, of which a
 // lane gets four rows' values of its column.
-// Bound: power and the vector and LDS work between matrix instructions.  16 384 rows, 4096 x 4096, bfloat16: 0.476 ms, 1.15 PFLOP/s, at
+// Bound: power and the vector and LDS work between matrix instructions.  16 384 rows, 4096 x 4096, bfloat16: 0.47 ms, 1.17 PFLOP/s, at
 // 1.84 GHz with the matrix units busy for 0.57 (zeros: 2.2 GHz, 0.41 ms; a library product of two bfloat16 matrices: 0.37); without
-// putting stages down 0.39, without reading operands either 0.31.  Rows of dY straight into LDS, three stages of them or 64 rows a stage
-// were no faster; waves of 128 x 128 spill.  A row's pieces of 16 columns (32 bytes) lie in the order u ^ turn_of(row), so that the
-// eight rows that a read touches are in different banks.
-// (rows of 64 columns are four pieces: two of the eight rows in the same banks)
+// putting stages down 0.39, without reading operands either 0.31.  Rows of dY straight into LDS or three stages of them were no faster;
+// 64 rows a stage pay for the two smaller tiles only, the square one's spill, and so do waves of 128 x 128.
+// A row's pieces of 16 columns (32 bytes) lie in the order u ^ turn_of(row), so that the eight rows that a read touches are in different
+// banks (rows of 64 columns are four pieces: two of the eight rows in the same ones).
 template <int ACROSS> __device__ inline int turn_of(int row) { return (2 * (row & 3) + ((row >> 2) & 1)) & (ACROSS / 16 - 1); }
 
 // (a closure that is called twice and not inlined keeps what it captures, the accumulators too, in memory)
@@ -962,9 +962,10 @@ __global__ __launch_bounds__(64 * WY * WX, 2) void f8_gradient_kernel(const Y *d
 
 // How a gradient is cut: which tile, and in how many parts the sum.  The larger tiles move half as much per operation, one at a time
 // on a CU; the wide one is for few columns of dY; two of the small ones run on a CU and leave half as many sums to be joined, and the
-// narrow one is for 64 columns and fewer.  The choice is the least of estimated times, from what the kernels were measured at.
-// (100 000 x 128 x 960 in float32: small tiles in 64 parts 110 us and 6 for their sums, wide ones in 125 parts 78 and 11; 1000 x 50 x 300:
-// small tiles in 16 parts 7.8 and 2, in 4 parts 12; 8410 x 56 x 4585 in 14 parts: small tiles 24.0, narrow ones 18.6.)
+// narrow one is for what would leave half of them empty.  The choice is the least of estimated times, from what the kernels were measured at.
+// (100 000 x 128 x 960 in float32: small tiles in 64 parts 110 us and 6 for their sums, wide ones in 125 parts 79 and 11; 1000 x 50 x 300 in
+// half precision: small tiles in 16 parts 7.8 and 2, in 4 parts 12, narrow ones in 16 parts 6.3 and 2; 8410 x 56 x 4585 in 14
+// parts: small tiles 24.0, narrow ones 18.6.)
 enum GradientKind { kSquare, kWide, kSmall, kNarrow };
 struct GradientShape {
     int kind, parts;
