@@ -61,9 +61,16 @@ def _format(dtype: torch.dtype) -> int:
     return _FORMAT[dtype]
 
 
+def _too_long(d: int):
+    # (a 32-bit argument of the library, which would take 2^32 + 5 for 5)
+    raise ValueError(f"{d} coordinates, columns or rows of weights: at most {MAX_D} are taken")
+
+
 def _table(t: F8Table):
     """Checks a table's tensors against one another; returns (its row count, its format)."""
     codes, scales, d = t
+    if d > MAX_D:
+        _too_long(d)
     n, nb = codes.shape[0], (d + 127) // 128
     form = _format(codes.dtype)
     if scales.dtype is not torch.uint8:
@@ -82,6 +89,8 @@ def _matrix(x: torch.Tensor):
     code = _efanna._mx_dtype(x.dtype)
     if not x.is_cuda or x.dim() != 2 or (x.numel() > 0 and x.shape[1] > 1 and x.stride(1) != 1):
         raise ValueError("expected a device matrix with dense rows")
+    if x.shape[1] > MAX_D:
+        _too_long(x.shape[1])
     return code, x.stride(0) if x.shape[0] > 1 else x.shape[1]
 
 
@@ -108,6 +117,8 @@ def efanna_f8_weights(W: torch.Tensor, form: torch.dtype = torch.float8_e4m3fn):
     same values: a layer's weights for the products of its forward and of its backward pass."""
     number, (code, ldw) = _format(form), _matrix(W)
     n, d = W.shape
+    if n > MAX_D:
+        _too_long(n)
     t, turned = _empty(n, d, form, W.device), _empty(d, n, form, W.device)
     lib()
     _efanna._call("efanna_f8_weights", W, W.data_ptr(), code, n, d, ldw, number, t.codes.data_ptr(), t.scales.data_ptr(),
