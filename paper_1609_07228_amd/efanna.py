@@ -335,9 +335,14 @@ def _mx_dtype(dtype: torch.dtype) -> int:
     return _MX_DTYPE[dtype]
 
 
+MX_MAX_D = 65536              # EFANNA_MX_MAX_D
+
+
 def _mx_table(t: MxTable) -> int:
     """Checks a table's tensors against one another; returns its row count."""
     codes, scales, norms, d = t
+    if d > MX_MAX_D:          # (also more than a 32-bit argument holds, which the library would not see)
+        raise EfannaError(-1, "MxTable")
     n, nb = codes.shape[0], (d + 31) // 32
     # (in few calls: a small table's kernel takes less time than its checks)
     if codes.dtype is not torch.uint8 or scales.dtype is not torch.uint8 or norms.dtype is not torch.float32:
@@ -365,6 +370,8 @@ def efanna_mx_quantise(X: torch.Tensor) -> MxTable:
     if not X.is_cuda or X.dim() != 2 or (X.numel() > 0 and X.shape[1] > 1 and X.stride(1) != 1):
         raise ValueError("expected a device matrix with dense rows")
     n, d = X.shape
+    if d > MX_MAX_D:
+        raise EfannaError(-1, "efanna_mx_quantise")
     ldx = X.stride(0) if n > 1 else d
     nb = (d + 31) // 32
     codes = torch.empty((n, 16 * nb), dtype=torch.uint8, device=X.device)
@@ -413,6 +420,8 @@ def efanna_mx_nearest(table: MxTable, queries: MxTable, k: int, first_self: int 
     n, nq = _mx_table(table), _mx_table(queries)
     if table.d != queries.d or table.codes.device != queries.codes.device:
         raise ValueError("the tables differ in their dimension or device")
+    if not -2 ** 31 <= k < 2 ** 31:
+        raise EfannaError(-1, "efanna_mx_nearest")
     device = table.codes.device
     ids = torch.empty((nq, max(k, 0)), dtype=torch.int32, device=device)
     dists = torch.empty((nq, max(k, 0)), dtype=torch.float32, device=device)
