@@ -7,6 +7,7 @@ import subprocess
 _HERE = os.path.dirname(os.path.abspath(__file__))
 SOURCES = [os.path.join(_HERE, "csrc", f) for f in ("trees.hip", "graph.hip", "search.hip", "mx.hip", "f8.hip")]
 HEADERS = [os.path.join(_HERE, "csrc", "common.h"), os.path.join(_HERE, "csrc", "tables.h"),
+           os.path.join(_HERE, "csrc", "pieces.h"),
            os.path.join(os.path.dirname(_HERE), "include", "efanna.h"),
            os.path.join(os.path.dirname(_HERE), "include", "efanna_f8.h")]
 LIB = os.path.join(_HERE, "libefanna_hip.so")

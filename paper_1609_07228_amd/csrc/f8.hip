@@ -3,6 +3,7 @@
 //
 // A power of two as a scale costs no precision (the codes are floating-point numbers themselves), and v_mfma_scale_f32_*_f8f6f4
 // applies it.  A row's blocks are whole, 128 bytes of codes each, so that every product is made of whole steps.
+#include "pieces.h"
 #include "tables.h"
 
 #include "../../include/efanna_f8.h"
@@ -761,23 +762,6 @@ struct GradientTile {
     static constexpr int lds = (int)sizeof(Lds) > waves * turn_bytes ? (int)sizeof(Lds) : waves * turn_bytes;
 };
 
-// Eight elements from the `by`-th on (the ones after the last: anything)
-template <class Y, class Eight> __device__ inline Eight moved_down(Eight x, int by)
-{
-    constexpr int kWords = 2 * sizeof(Y);
-    typedef u32 Words __attribute__((ext_vector_type(kWords)));
-    Words w = __builtin_bit_cast(Words, x);
-    const int words = by * (int)sizeof(Y) / 4;
-#pragma unroll
-    for (int bit = 1; bit < kWords; bit *= 2)
-#pragma unroll
-        for (int k = 0; k + bit < kWords; ++k) w[k] = words & bit ? w[k + bit] : w[k];
-    if (sizeof(Y) == 2)
-#pragma unroll
-        for (int k = 0; k < kWords; ++k) w[k] = by & 1 ? w[k] >> 16 | (k + 1 < kWords ? w[k + 1] << 16 : 0) : w[k];
-    return __builtin_bit_cast(Eight, w);
-}
-
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef short i16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
@@ -809,7 +793,7 @@ __global__ __launch_bounds__(64 * WY * WX, 2) void f8_gradient_kernel(const Y *d
     // matrix of fewer columns is read one by one)
     const bool pieces_whole = n % 8 == 0;
     const int col_y = tid % (Tile::across_y / 8) * 8, row_y = tid / (Tile::across_y / 8), rows_y = Tile::threads / (Tile::across_y / 8);
-    const int from_col = n >= 8 ? min(j0 + col_y, n - 8) : 0;      // 0 at least
+    const int from_col = piece_from(j0 + col_y, n);      // 0 at least
     const int piece_x = min(c0 / 16 + tid % (Tile::across_x / 16), x.nb * 8 - 1), row_x = tid / (Tile::across_x / 16),
               rows_x = Tile::threads / (Tile::across_x / 16);
     const auto load_y = [&](int stage, int set, int i, auto inside) EF_INLINE {
@@ -819,7 +803,7 @@ __global__ __launch_bounds__(64 * WY * WX, 2) void f8_gradient_kernel(const Y *d
         if (inside || n >= 8) raw_y[set][i] = *(const Eight *)(from + (offset + from_col));
         else
 #pragma unroll
-            for (int k = 0; k < 8; ++k) raw_y[set][i][k] = from[offset + min(k, n - 1)];
+            for (int k = 0; k < 8; ++k) raw_y[set][i][k] = from[offset + piece_column(k, n)];
     };
     const auto load_x = [&](int stage, int set, int i) EF_INLINE {
         const int at = min(stage, stages - 1) * STEP, row = min(row_x + rows_x * i, rows_in - 1 - at);
@@ -832,7 +816,7 @@ __global__ __launch_bounds__(64 * WY * WX, 2) void f8_gradient_kernel(const Y *d
         const bool live = stage * STEP + row < rows_in;
         bf16x8 part[Tile::parts];
         Eight x = live ? raw_y[set][i] : (Eight)(Y)0.0f;
-        if (!inside) x = moved_down<Y>(x, n >= 8 ? j0 + col_y - from_col : 0);
+        if (!inside) x = moved_down<Y>(x, piece_moved(j0 + col_y, n));
         Parts<Y>::split(x, part);
 #pragma unroll
         for (int q = 0; q < Tile::parts; ++q) *(bf16x8 *)&lds.y[buffer][q][row][((piece >> 1) ^ turn_of<Tile::across_y>(row)) * 16 + (piece & 1) * 8] = part[q];
