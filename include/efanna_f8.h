@@ -13,7 +13,8 @@
  *   codes  n * 128 * nb bytes, 16-byte aligned.
  *   scales n * sp bytes, sp = nb rounded up to a multiple of 4, 4-byte aligned; padding bytes 0.
  * A value is code * scale, exactly; one of 2^128 (which the largest float32 numbers are rounded to) reads
- * as an infinity in every type.
+ * as an infinity in every type, and is one in gradients and in products to float32 (products to 16 bits take
+ * it as 2^128).
  * 1 <= d <= EFANNA_F8_MAX_D, n < 2^31 - 65536.  Row counts may be 0 (pointers to what has no elements
  * may be NULL).  Element types of other matrices: EFANNA_F32, EFANNA_F16 or EFANNA_BF16, aligned to
  * their size.  All calls are asynchronous on `stream`, can be captured into a graph, and allocate
