@@ -2,7 +2,8 @@
 each block of 128.
 
 Argument marshalling only, as in `efanna`: every step runs in the HIP kernels of libefanna_hip.so on the current stream
-of the GPU that holds the tensors, and there is no CPU fallback.
+of the GPU that holds the tensors, and there is no CPU fallback.  Calls record nothing for autograd: results have no gradients,
+whatever the arguments ask for; a layer is an autograd function around them (examples/f8_projection.py has one).
 """
 from __future__ import annotations
 
