@@ -61,8 +61,9 @@ int efanna_f8_rows(const uint8_t *codes, const uint8_t *scales, int32_t format, 
  * 2^-133).  For 16-bit results the matrix units take 8-bit operands, whose products they add in groups of eight,
  * each product cut off at 2^-14 of its group's largest: at most 2^-11 of the sum of magnitudes is lost.  Of sums of
  * a thousand and more random terms two to three in a hundred were then a step of their type beside the nearest
- * number, and the error against exact sums 0.2 % larger at most; sums whose terms cancel are better taken to
- * EFANNA_F32 and converted.
+ * number, and the error against exact sums 0.2 % larger at most; sums of terms of one sign came out smaller by 3e-6
+ * of them, of terms of very different size by 1e-4.  Sums whose terms cancel are better taken to EFANNA_F32 and
+ * converted.
  * ws     [device] 256-byte aligned, efanna_f8_product_workspace_bytes bytes; may be NULL where that is 0.
  * EFANNA_EUNSUPPORTED for what one launch does not take: 2^23 tiles of 256 x 256 and more (half a terabyte of
  * output). */
